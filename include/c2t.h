@@ -39,7 +39,8 @@ extern "C" {
 
 typedef struct c2t_ctx c2t_ctx;
 
-typedef enum { C2T_F32 = 0, C2T_BF16 = 1 } c2t_dtype;
+/* C2T_F16: keys and values of a cache only (c2t_cache); logits are C2T_F32 or C2T_BF16. */
+typedef enum { C2T_F32 = 0, C2T_BF16 = 1, C2T_F16 = 2 } c2t_dtype;
 /* C2T_CLS_MLP: the paper's two-layer FFN.  C2T_CLS_IDENTITY_JOINT: confidence := joint
  * probability, which turns the method into EAGLE-2's expand + rerank (Sec. 2.2) and, with
  * K = F = 1, into the "DyJoint" early-stop rule of the chain-mode comparison (Sec. 5, Benefits
@@ -81,6 +82,10 @@ typedef enum { C2T_ADD_FRONTIER = 0, C2T_ADD_ALL_SURVIVORS = 1 } c2t_tree_add;
  * never made).  The results of the sequence in this step are unspecified; later steps are not affected.
  * Never set by data. */
 #define C2T_ST_INTERNAL      16u
+/* Of a cache's status words (c2t_cache): the pool had no free page left; a length, slot, path or page number was out of range
+ * (the access is skipped, never made). */
+#define C2T_ST_NO_PAGE       32u
+#define C2T_ST_BAD_PAGE      64u
 
 /*
  * Method parameters (Alg. 1's inputs d_max and beta; Top-K of Sec. 4.2.2 split into the
@@ -469,6 +474,177 @@ size_t c2t_host_step_ints(const c2t_config *cfg);
  * c2t_accept_lazy the pinned buffer.)
  */
 int c2t_decode_step_host(c2t_ctx *ctx, const c2t_host_step *io, void *stream);
+
+/*
+ * The paged key/value cache that a tree's verification reads (tree attention, Sec. 2.2): the target model attends every final
+ * node to its sequence's prefix and to the node's ancestors, in one pass over keys and values that lie in pages.  The calls
+ * below need no context: they take this description, whose arrays all belong to the caller, work on the device that is
+ * current, only enqueue work on `stream` and neither allocate nor synchronise.  A step of a layer is
+ *
+ *   c2t_cache_reserve(prefix_len + n_nodes)              once: pages for the nodes
+ *   per layer:  c2t_cache_append(layer, K, V of the nodes, prefix_len, n_nodes)      node j lies at prefix_len + j
+ *               c2t_verify_attention(layer, Q of the nodes, mask_bits of c2t_build_verify)
+ *   c2t_accept
+ *   c2t_cache_compact(prefix_len, accept_len, path)      once: the accepted nodes move to the front, in all layers
+ *   c2t_cache_release(new lengths)                       once: the pages behind them go back
+ *
+ * A page holds page_size tokens of all layers and heads; position p of slot b lies in page table[b][p / page_size], place
+ * p % page_size.  refs counts the slots that hold a page: 0 = free.  Free pages are always taken in ascending order, for the slots in
+ * ascending order, so that equal calls leave equal tables.  A fresh cache is: refs 0, held 0, status 0; the library
+ * never reads entries of table at or past held.  Pages below a fork's length are shared by the slots that hold them; whoever
+ * writes at or past its own length therefore writes to pages that nobody else holds.
+ * Calls on one cache must be ordered (one stream, or events), as those of a context.
+ */
+#define C2T_MAX_PAGE_SIZE 256
+typedef struct {
+  int32_t dtype;                /* C2T_BF16 or C2T_F16                                                  */
+  int32_t batch;                /* B slots, at most C2T_MAX_BATCH                                       */
+  int32_t layers, kv_heads;
+  int32_t head_dim;             /* 64 or 128                                                            */
+  int32_t page_size;            /* a power of two, 8 to C2T_MAX_PAGE_SIZE                               */
+  int32_t n_pages;              /* pages of the pool                                                    */
+  int32_t max_pages;            /* pages of one slot at most: width of a table row                      */
+  void *k_dev, *v_dev;          /* element offset of (layer, page, place, head, d) = layer*layer_stride +
+                                   page*page_stride + place*token_stride + head*head_stride + d; bases
+                                   16-byte aligned, strides multiples of 16 bytes                       */
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  int32_t *table_dev;           /* [B, max_pages]                                                       */
+  int32_t *held_dev;            /* [B] pages that a slot holds                                          */
+  int32_t *refs_dev;            /* [n_pages]                                                            */
+  uint32_t *status_dev;         /* [B] C2T_ST_* bits, only ever ORed; NULL = not wanted                 */
+} c2t_cache;
+
+/*
+ * Makes every slot hold pages for at least len_dev[b] tokens ([B] int32).  Slots that hold enough are left alone.  Where the free
+ * pages run out the first slot whose need is not met and all later ones with a need get none and C2T_ST_NO_PAGE; a length
+ * below 0 or beyond max_pages * page_size sets C2T_ST_BAD_PAGE and the slot is left as it was.  One launch.
+ */
+int c2t_cache_reserve(const c2t_cache *cache, const int32_t *len_dev, void *stream);
+
+/*
+ * Gives back the pages behind the first keep_len_dev[b] tokens of every slot ([B] int32; 0 = all of them): their counts drop by
+ * one and their table entries become -1.  A length that reaches past the held pages keeps them all; a negative one sets
+ * C2T_ST_BAD_PAGE.  One launch.
+ */
+int c2t_cache_release(const c2t_cache *cache, const int32_t *keep_len_dev, void *stream);
+
+/*
+ * Forks slots: every slot b with src_dev[b] >= 0 becomes a copy of the first len_dev[b] tokens of slot src_dev[b].  Whole pages are
+ * shared (their counts rise), a page that is only begun is copied, in all layers, to a free page.  Slot b must be empty
+ * (held 0), slot src_dev[b] must hold the tokens and must not be forked into by the same call; several slots may fork the same one.
+ * Otherwise, or where no free page is left, the slot stays empty and gets C2T_ST_BAD_PAGE or C2T_ST_NO_PAGE.
+ * forked_dev [B] int32, an array of its own: 1 for the slots that were made, 0 for all others.  Two launches.
+ */
+int c2t_cache_fork(const c2t_cache *cache, const int32_t *src_dev, const int32_t *len_dev, int32_t *forked_dev, void *stream);
+
+/*
+ * Writes the keys and values of new tokens to their pages: token j < count_dev[b] of slot b goes to position start_dev[b] + j of
+ * `layer`.  k_new_dev / v_new_dev: [B, max_new, kv_heads, head_dim] of the cache's dtype, element offset b*seq_stride + j*token_stride +
+ * h*head_stride + d (16-byte aligned, as in c2t_cache).  A token whose position has no held page is skipped and sets
+ * C2T_ST_BAD_PAGE.  One launch.
+ */
+int c2t_cache_append(const c2t_cache *cache, int32_t layer, const void *k_new_dev, const void *v_new_dev, int32_t max_new,
+                     int64_t seq_stride, int64_t token_stride, int64_t head_stride, const int32_t *start_dev,
+                     const int32_t *count_dev, void *stream);
+
+/*
+ * Keeps the accepted path (Sec. 5 Metrics) and drops the tree's other nodes: in every layer the keys and values at position
+ * prefix_len[b] + path[b][d] move to prefix_len[b] + d, d = 0 .. accept_len[b].  accept_len_dev [B] and path_dev [B, path_width]
+ * as c2t_accept writes them (node ids ascending along the path; path_width = D + 1, at most C2T_MAX_DEPTH + 1).
+ * new_len_dev [B] (an array of its own, may be NULL): prefix_len + accept_len + 1, the next step's prefix and what c2t_cache_release wants.  A path that is not
+ * ascending, or leaves the held pages, sets C2T_ST_BAD_PAGE; that slot is left as it was and new_len is its prefix_len.  One launch.
+ */
+int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, const int32_t *accept_len_dev,
+                      const int32_t *path_dev, int32_t path_width, int32_t *new_len_dev, void *stream);
+
+/*
+ * Attention of new tokens over the cache (Sec. 2.2).  Query i < n_queries[b] of slot b is tree node i (or token i of a chunk), whose
+ * own key lies at position prefix_len[b] + i.  With S(i) the positions that it sees,
+ *
+ *   out[b, i, h] = sum_{p in S(i)} w_p v_p,   w = softmax over S(i) of scale * (q . k_p),   lse[b, i, h] = ln sum exp(scale * (q . k_p))
+ *
+ * S(i) = the prefix [0, prefix_len[b]) and
+ *   with mask_bits:     the nodes j whose bit is set in row i of mask_bits [B, max_queries, mask_words] (c2t_build_verify's);
+ *                       nodes at or past mask_words * 64 are not seen;
+ *   without (NULL):     the tokens j <= i (a causal chunk; max_queries = 1 is plain decoding).
+ * window > 0 keeps of these the positions less than `window` before the query's own, and the first `sinks` positions, which stay visible.
+ * A node's own position is position_ids[b, i] (c2t_build_verify's; NULL: prefix_len + i; a value below prefix_len[b] counts as
+ * prefix_len[b]).  A row that sees nothing gets zeros and lse = -inf.  Keys and values that no mask lets a row see do not reach it,
+ * whatever they hold (NaN and infinities included).
+ * Query head h reads key head h / (q_heads / kv_heads).  Rows i >= n_queries[b] are neither read nor written.
+ * n_queries is cut to max_queries; positions without a held page are not seen (C2T_ST_BAD_PAGE).  A page number out of range among the
+ * held ones sets that bit too and leaves the slot's rows unspecified, but nothing out of bounds is touched.
+ * Products are of 16 bits with 32-bit sums; the weights are rounded to the cache's type for the second product.
+ */
+typedef struct {
+  int32_t layer;
+  int32_t q_heads;              /* a multiple of kv_heads                                               */
+  int32_t max_queries;          /* Nq: query slots per sequence                                         */
+  const void *q_dev;            /* [B, Nq, q_heads, head_dim] of the cache's dtype                      */
+  void *out_dev;                /* the same shape and type, strides of its own                          */
+  int64_t q_seq_stride, q_token_stride, q_head_stride;         /* elements, multiples of 16 bytes       */
+  int64_t out_seq_stride, out_token_stride, out_head_stride;
+  float *lse_dev;               /* [B, Nq, q_heads] contiguous, or NULL                                 */
+  const int32_t *n_queries_dev; /* [B]                                                                  */
+  const int32_t *prefix_len_dev;/* [B]                                                                  */
+  const uint64_t *mask_bits_dev;
+  int32_t mask_words;
+  const int32_t *position_ids_dev;   /* [B, Nq] or NULL                                                 */
+  int32_t window, sinks;        /* 0 = no window; sinks >= 0                                            */
+  float scale;
+} c2t_attention;
+
+/* Workspace of c2t_verify_attention for such a call (0 on invalid sizes): the parts of rows whose keys are read by several thread
+ * blocks.  It needs no clearing and holds nothing between calls; calls that may overlap need one each. */
+size_t c2t_verify_attention_workspace_bytes(const c2t_cache *cache, int32_t q_heads, int32_t max_queries);
+int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention, void *workspace_dev, size_t workspace_bytes,
+                         void *stream);
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on logits rows, before a level or an acceptance walk reads them; draft and
+ * target rows need the same ones, or the walk stops early.  A row belongs to a tree node, whose text is the sequence's history and the
+ * tokens on the node's own root path.  With c(v) = counts[b, v] + the nodes on that path with token v,
+ *
+ *   x = in[b, r, v]
+ *   c > 0:  x = x > 0 ? x / repetition[b] : x * repetition[b];   x -= frequency[b] * c;   x -= presence[b]
+ *   x += bias[b, v]
+ *   out[b, r, v] = allowed(b, r, v) ? x : -inf            (rounded once; a token that is not allowed gets -inf whatever its logit)
+ *
+ * computed in fp32.  Each of the arrays may be NULL: no history, factor 1, penalties 0, bias 0, all tokens allowed, no tree.
+ * in_dev and out_dev: [B, rows, vocab] of dtype (C2T_F32 or C2T_BF16), bases and strides as for c2t_expand_level; they may be the
+ * same array with the same strides, or must not overlap.  Rows r >= n_rows[b] are neither read nor written.
+ * For target rows: node_* = c2t_verify's tokens and parents, row_node NULL (row r is node r).  For the rows of a level: the tree's arrays of
+ * c2t_get_view and c2t_frontier's node_id.
+ */
+typedef struct {
+  int32_t dtype, batch, rows, vocab;
+  const void *in_dev;
+  void *out_dev;
+  int64_t in_seq_stride, in_row_stride, out_seq_stride, out_row_stride;      /* elements                 */
+  const int32_t *n_rows_dev;    /* [B]; NULL: all rows                                                  */
+  const int32_t *counts_dev;    /* [B, vocab], row stride counts_stride; how often the history has a token (>= 0) */
+  int64_t counts_stride;
+  const float *repetition_dev, *frequency_dev, *presence_dev;                /* [B] each                 */
+  const float *bias_dev;        /* [B, vocab], row stride bias_stride; 0: one table for all             */
+  int64_t bias_stride;
+  const uint32_t *allowed_dev;  /* bit v % 32 of word v / 32 of row (b, r), at b*allowed_seq_stride + r*allowed_row_stride words */
+  int64_t allowed_seq_stride, allowed_row_stride;
+  int32_t nodes;                /* N: width of the node arrays, at most C2T_MAX_TREE                    */
+  const int32_t *node_token_dev, *node_parent_dev;                           /* [B, N]; parent -1: none  */
+  const int32_t *row_node_dev;  /* [B, rows] the node of each row; < 0 or >= N: none; NULL: row r is node r */
+} c2t_logit_rules;
+/* A root path is followed over C2T_MAX_DEPTH + 1 nodes at most.  One launch. */
+int c2t_penalize_logits(const c2t_logit_rules *rules, void *stream);
+
+/*
+ * counts[b, tokens[b, index[b, k]]] += delta for k < n_dev[b], at most `width` of them: with c2t_verify's tokens and c2t_accept's path
+ * as the index (index row stride index_stride) this takes the accepted tokens into the history; index NULL counts tokens[b, k].  Entries of
+ * index outside [0, token_width) and tokens outside [0, vocab) are skipped.  plus_one = 1 counts n_dev[b] + 1 entries (accept_len excludes the
+ * root).  One launch.
+ */
+int c2t_count_tokens(int32_t *counts_dev, int64_t counts_stride, int32_t batch, int32_t vocab, const int32_t *tokens_dev,
+                     int32_t token_width, const int32_t *index_dev, int32_t index_stride, const int32_t *n_dev, int32_t plus_one,
+                     int32_t width, int32_t delta, void *stream);
 
 /* Number of kernels the context has launched since c2t_init (host-side counter). */
 int64_t c2t_launch_count(const c2t_ctx *ctx);

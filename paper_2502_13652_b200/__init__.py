@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     OK, EINVAL, EALIGN, ERANGE, EORDER, ECUDA, ENOMEM,
     ST_NAN_LOGIT, ST_POSINF_LOGIT, ST_ALL_NEGINF, ST_TREE_OVERFLOW, ST_INTERNAL,
 )
+from .kv_cache import (  # noqa: F401,E402
+    KVCache, c2t_penalize_logits, c2t_count_tokens, F16, ST_NO_PAGE, ST_BAD_PAGE)
 from .weights import save_classifier, load_classifier  # noqa: F401,E402
 from .vocab_parallel import (  # noqa: F401,E402
     shard_ranges, gather_row_records, vocab_parallel_level, vocab_parallel_accept, vocab_parallel_accept_lazy,
