@@ -67,6 +67,15 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *r) {
                "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
                ::C2T_W4(r, 0), C2T_W4(r, 4), C2T_W4(r, 8), C2T_W4(r, 12), C2T_W4(r, 16), C2T_W4(r, 20), C2T_W4(r, 24), C2T_W4(r, 28), "r"(at) : "memory");
 }
+// 16 columns
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t *r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : C2T_R4(r, 0), C2T_R4(r, 4), C2T_R4(r, 8), C2T_R4(r, 12) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::C2T_W4(r, 0), C2T_W4(r, 4), C2T_W4(r, 8), C2T_W4(r, 12), "r"(at) : "memory");
+}
 #undef C2T_R4
 #undef C2T_W4
 

@@ -250,7 +250,7 @@ __device__ __forceinline__ int place_of_values(int t, int n, int ahead) { return
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
 // which of the 32 keys from `key` row i sees
-__device__ uint32_t sight_bits(const Sight &s, int i, int own, int key) {
+__device__ __forceinline__ uint32_t sight_bits(const Sight &s, int i, int own, int key) {
   uint32_t on = low_bits(s.keys - key);
   const int node = key - s.prefix;          // of the first of them
   const uint32_t cached = low_bits(-node);
@@ -547,9 +547,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       const int own = see.position(node);
       float m = -INFINITY, l = 0.f;
       for (int t = two ? 0 : s; t < n; t += ahead) {
+        const int key = w.key0(x.k0 + t);
+        const bool all = key + kTile <= see.prefix && key + kTile <= see.keys && (see.window == 0 || key > own - see.window || key + kTile <= see.sinks);
+        const bool masked = !__all_sync(~0u, all);
+        uint32_t on0 = ~0u, on1 = ~0u, on2 = ~0u, on3 = ~0u;
+        if (masked && warp_live) {          // (while the logits are on their way)
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            on0 = on1; on1 = on2; on2 = on3;
+            on3 = sight_bits(see, node, own, key + 32 * i);
+          }
+        }
         if (!(ok = wait(sh, sh.logits + s, logits_turn++ & 1))) break;
         tmem_fence_after();
-        const int key = w.key0(x.k0 + t);
         if (key + kTile > see.keys) {       // rows of the values that nobody wrote: their weights are 0, they must be numbers
           const int at_v = turn + place_of_values(t, n, ahead);
           if (!(ok = wait(sh, sh.full + at_v % kRing, at_v / kRing & 1))) break;
@@ -562,26 +572,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         }
         __syncwarp();
         if (warp_live) {
-          uint32_t r[kTile];
+          // 32 logits at a time, and once more for the weights: to read tensor memory twice is cheaper than 128 registers
+          uint32_t r[2][32];
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          tmem_load32(my_s, r[0]);
 #pragma unroll
-          for (int i = 0; i < kTile; i += 32) tmem_load32(my_s + i, r + i);
-          tmem_wait_loads();
-          float *x_ = reinterpret_cast<float *>(r);
-          const bool all = key + kTile <= see.prefix && key + kTile <= see.keys && (see.window == 0 || key > own - see.window || key + kTile <= see.sinks);
-          if (!__all_sync(~0u, all)) {
+          for (int i = 0; i < 4; ++i) {
+            tmem_wait_loads();
+            if (i < 3) tmem_load32(my_s + 32 * (i + 1), r[(i + 1) & 1]);
+            const uint32_t on = i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3;
+            uint32_t *y = r[i & 1];
+            if (masked) {
 #pragma unroll
-            for (int i = 0; i < kTile; i += 32) {
-              const uint32_t on = sight_bits(see, node, own, key + i);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) x_[i + j] = on >> j & 1 ? x_[i + j] : -INFINITY;
+              for (int j = 0; j < 32; ++j) y[j] = on >> j & 1 ? y[j] : 0xFF800000u;
             }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(y[j]));
           }
-          __syncwarp();
-          float top[4] = {x_[0], x_[1], x_[2], x_[3]};
-#pragma unroll
-          for (int i = 4; i < kTile; i += 4)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], x_[i + j]);
+          tmem_load32(my_s, r[0]);
           const float highest = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
           // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
           const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
@@ -589,29 +597,38 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           if (raise) { l *= factor; m = highest; }
           if (__any_sync(~0u, raise) && t >= ahead) {
 #pragma unroll
-            for (int i = 0; i < D; i += 32) {
-              uint32_t o[32];
-              tmem_load32(my_o + i, o);
+            for (int i = 0; i < D; i += 16) {
+              uint32_t o[16];
+              tmem_load16(my_o + i, o);
               tmem_wait_loads();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
-              tmem_store32(my_o + i, o);
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
+              tmem_store16(my_o + i, o);
             }
           }
           const float shift = m == -INFINITY ? 0.f : m * unit;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < kTile; i += 4)
+          for (int i = 0; i < 4; ++i) {
+            tmem_wait_loads();
+            if (i < 3) tmem_load32(my_s + 32 * (i + 1), r[(i + 1) & 1]);
+            const uint32_t on = i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3;
+            uint32_t *y = r[i & 1];
+            if (masked) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              x_[i + j] = exp2_fast(fmaf(x_[i + j], unit, -shift));
-              sum[j] += x_[i + j];
+              for (int j = 0; j < 32; ++j) y[j] = on >> j & 1 ? y[j] : 0xFF800000u;
             }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            uint32_t packed[16];
 #pragma unroll
-          for (int i = 0; i < kTile / 2; ++i) r[i] = pack<T>(x_[2 * i], x_[2 * i + 1]);
-          tmem_store32(my_s, r);
-          tmem_store32(my_s + 32, r + 32);
+            for (int j = 0; j < 32; j += 2) {
+              const float lo = exp2_fast(fmaf(__uint_as_float(y[j]), unit, -shift)), hi = exp2_fast(fmaf(__uint_as_float(y[j + 1]), unit, -shift));
+              sum[j & 2] += lo;
+              sum[(j & 2) + 1] += hi;
+              packed[j / 2] = pack<T>(lo, hi);
+            }
+            tmem_store16(my_s + 16 * i, packed);                // over logits that have been read
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tmem_wait_stores();
         }
         tmem_fence_before();
