@@ -7,6 +7,15 @@ namespace c2t {
 
 __device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// one lane of a whole warp, the same one every time
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes;
+}
+// a value that all lanes of the warp have, in a register that they share
+__device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(~0u, x); }
+
 // ---------------------------------------------------------------- barriers in shared memory
 
 __device__ __forceinline__ void barrier_init(uint64_t *bar, int arrivals) {

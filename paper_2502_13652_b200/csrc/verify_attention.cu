@@ -107,6 +107,7 @@ struct Params {
   c2t_cache c;
   c2t_attention a;
   int group, blocks_per_seq;                // query heads of a key head; blocks of max_queries * group rows
+  uint32_t group_inverse;                   // 2^32 / group, rounded up (group > 1)
   int box_rows;                             // tokens of one copy: a page's, at most a tile's
   int split;                                // 1: tiles are dealt out evenly, blocks of rows may be cut; 0: whole blocks
   float *part_o;                            // [2 G][kBlockRows][D]: unfinished sums over the values, two per thread block
@@ -114,26 +115,28 @@ struct Params {
   int4 *cut;                                // [G]: {pair, key head, first thread block, last} of a cut block of rows
 };
 
+// row -> (new token, query head of the group); rows * group < 2^32, which makes the inverse exact
+__device__ __forceinline__ int token_of(const Params &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_inverse); }
+
 struct Maps { TensorMap k, v; };
 
-struct Block {
-  Sight see;
-  int b, row0, rows;                        // first row; rows that are there
-  int sink_tiles, first_tile, tiles;
+struct Block {                              // with the tiles [k0, k1) of it that a thread block takes
+  int b, head, row0, rows;                  // key head; first row; rows that are there (0: no block)
+  int prefix, n, keys;                      // of the sequence, as in Sight
+  int sink_tiles, first_tile, tiles, k0, k1;
   __device__ __forceinline__ int key0(int t) const { return (t < sink_tiles ? t : first_tile + t - sink_tiles) * kTile; }
 };
 
 __device__ __forceinline__ Block block_of(const Params &p, int pair) {
   Block w;
-  w.b = pair / p.blocks_per_seq;
+  w.b = p.blocks_per_seq == 1 ? pair : pair / p.blocks_per_seq;
   w.row0 = (pair - w.b * p.blocks_per_seq) * kBlockRows;
-  w.see = sight_of(p.c, p.a, w.b);
-  const Sight &s = w.see;
-  const long long all = (long long)s.n * p.group;
-  w.rows = (int)min(max(all - w.row0, 0ll), (long long)kBlockRows);
-  w.sink_tiles = w.first_tile = w.tiles = 0;
+  const Sight s = sight_of(p.c, p.a, w.b);
+  w.prefix = s.prefix; w.n = s.n; w.keys = s.keys;
+  w.rows = min(max(s.n * p.group - w.row0, 0), kBlockRows);
+  w.sink_tiles = w.first_tile = w.tiles = w.head = w.k0 = w.k1 = 0;
   if (w.rows == 0) return w;
-  const int first = w.row0 / p.group, last = (w.row0 + w.rows - 1) / p.group;
+  const int first = token_of(p, w.row0), last = token_of(p, w.row0 + w.rows - 1);
   const int end = s.bits ? s.keys : min(s.keys, s.prefix + last + 1);
   const int end_tile = (end + kTile - 1) / kTile;
   if (s.window > 0) {
@@ -145,88 +148,71 @@ __device__ __forceinline__ Block block_of(const Params &p, int pair) {
   return w;
 }
 
-// The thread block's share: a walk over (pair, key head, tiles).  Every role of the block makes the same one.
-struct Walk {
-  long long left;                           // tiles to go (dealt out) or pairs-and-heads (whole blocks)
-  int pair, head, k0, k1;
-  Block w;
+__device__ __forceinline__ Sight sight_of(const Params &p, const Block &w) {
+  Sight s;
+  s.prefix = w.prefix; s.n = w.n; s.keys = w.keys;
+  s.window = p.a.window;
+  s.sinks = p.a.sinks;
+  s.words = p.a.mask_words;
+  s.bits = p.a.mask_bits_dev ? p.a.mask_bits_dev + (long long)w.b * p.a.max_queries * p.a.mask_words : nullptr;
+  s.positions = p.a.position_ids_dev ? p.a.position_ids_dev + (long long)w.b * p.a.max_queries : nullptr;
+  return s;
+}
+
+// An even deal of `total` tiles to `used` thread blocks: the first `more` of them get one more than the others.
+struct Deal {
+  long long total;
+  int used, more;
+  long long each;
+  __device__ __forceinline__ Deal(long long total_, int grid) : total(total_) {
+    used = (int)min(max(total, 1ll), (long long)grid);          // (none without a tile)
+    each = total < 0x7FFFFFFF ? (uint32_t)total / (uint32_t)used : total / used;
+    more = (int)(total - each * used);
+  }
+  __device__ __forceinline__ long long begin(int c) const { return c >= used ? total : c * each + min(c, more); }
+  __device__ __forceinline__ int owner(long long x) const {     // of tile x
+    const long long wide = more * (each + 1), y = x < wide ? x : x - wide, by = x < wide ? each + 1 : each;
+    return (x < wide ? 0 : more) + (int)(y < 0x7FFFFFFF ? (uint32_t)y / (uint32_t)by : y / by);
+  }
 };
-
-__device__ __forceinline__ bool walk_load(const Params &p, Walk &x, int n_pairs) {        // to the next pair that has rows
-  while (x.pair < n_pairs) {
-    x.w = block_of(p, x.pair);
-    if (x.w.tiles > 0) return true;
-    ++x.pair;
-  }
-  return false;
-}
-
-// Makes [k0, k1) the next tiles; false at the end.
-__device__ __forceinline__ bool walk_next(const Params &p, Walk &x, int n_pairs, bool first) {
-  if (p.split) {
-    if (!first) {
-      x.left -= x.k1 - x.k0;
-      if (x.left <= 0) return false;
-      x.k0 = 0;
-      if (++x.head == p.c.kv_heads) {
-        x.head = 0;
-        ++x.pair;
-        if (!walk_load(p, x, n_pairs)) return false;
-      }
-    } else if (x.left <= 0) {
-      return false;
-    }
-    x.k1 = (int)min((long long)x.w.tiles, x.k0 + x.left);
-    return true;
-  }
-  long long item = first ? blockIdx.x : x.left + gridDim.x;
-  for (; item < (long long)n_pairs * p.c.kv_heads; item += gridDim.x) {
-    const int pair = (int)(item / p.c.kv_heads);
-    if (first || pair != x.pair) x.w = block_of(p, pair);
-    x.pair = pair;
-    x.head = (int)(item - (long long)pair * p.c.kv_heads);
-    first = false;
-    if (x.w.tiles > 0) {
-      x.left = item;
-      x.k0 = 0;
-      x.k1 = x.w.tiles;
-      return true;
-    }
-  }
-  return false;
-}
 
 // ---------------------------------------------------------------- the kernel
 // Two accumulators of 128 rows, each with a group of four warps that takes its logits through the softmax.  A block of more than 128
 // rows has its halves in them, which read the same tiles; a smaller one goes over its tiles with both, the even ones and the odd ones, and
 // adds up at the end.  Either way one group's exponentials run while the tensor cores work for the other.
-//   warp 8   issues the products: logits S = Q K^T (both from shared memory), and O += P V with P, the weights, in tensor memory in S's place
-//   warp 9   copies the tiles of keys and values, a box per page and 64 elements of a head, into a ring of buffers
 //   warps 0-3, 4-7   a thread per row: S from tensor memory, its maximum, the weights back as 16-bit numbers
+//   warp 8    issues the products: logits S = Q K^T (both from shared memory), and O += P V with P, the weights, in tensor memory in S's place
+//   warp 9    copies the tiles of keys and values, a box per page and 64 elements of a head, into a ring of buffers
+//   warp 10   walks through the thread block's share and describes the next blocks of rows to the others
 // The running maximum is only raised when a row's new one is more than 2^8 in weight above it: then O and the sum are rescaled.  Weights
 // are so at most 2^8, which both types hold.
+// Up to 32 (64) rows lie in the accumulator four times (twice), and each copy takes a quarter (half) of a tile's keys, with weights of 0
+// for the others: all warps have work then, and a tile's softmax, which is what such a block waits for, a quarter of the steps.
 
-constexpr int kSoftmaxThreads = 256, kThreads = 320;
+constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x 128 at most
 constexpr float kRaise = 8.f;
 constexpr int kTries = 1 << 22;             // of a wait, after which the block gives up
 
 template <int D> struct Ring { static constexpr int bytes = kTile * D * 2, n = D == 128 ? 5 : 10; };
 
+constexpr int kBlocks = 4;                  // descriptions ahead
+constexpr int kReaders = 10;                // warps that read them
+
 template <int D>
 struct alignas(1024) Shared {
-  unsigned char q[2][kRows * D * 2];        // 64 elements of all rows after the other 64
+  unsigned char q[2][kRows * D * 2];        // 64 elements of all rows after the other 64; at a block's end its sums over the values
   union {
     unsigned char ring[Ring<D>::n][Ring<D>::bytes];
     long long before[C2T_MAX_BATCH + 1];    // while the work is dealt out: tiles of the pairs before
   };
   float2 ml[2][kRows];
   uint64_t full[Ring<D>::n], empty[Ring<D>::n];
-  uint64_t logits[2], weights[2], done, queries, halves;
+  uint64_t logits[2], weights[2], done, queries, meet, described[kBlocks], read[kBlocks];
+  Block block[kBlocks];
   uint32_t tmem;
   int gave_up;
-  long long warp_sum[kThreads / 32];
-  long long left;
+  long long warp_sum[kThreads / 32], left;
   int pair, head, k0;
 };
 
@@ -242,9 +228,18 @@ __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t pari
   return false;
 }
 
-// place of a tile's keys or values in the order of the copies: K_0 .. K_{ahead-1}, then V_t, K_{t+ahead}
-__device__ __forceinline__ int place_of_keys(int t, int ahead) { return t < ahead ? t : 2 * t - ahead + 1; }
-__device__ __forceinline__ int place_of_values(int t, int n, int ahead) { return min(n, ahead + t) + t; }
+// A buffer of the ring and the parity of its barriers.  The copies' order: K_0 .. K_{ahead-1}, then V_t, K_{t+ahead} in turn.
+template <int n>
+struct Cursor {
+  int at;
+  uint32_t parity;
+  __device__ __forceinline__ void step(int by) {                // by < n
+    at += by;
+    if (at >= n) { at -= n; parity ^= 1; }
+  }
+};
+__device__ __forceinline__ int step_of_keys(int t, int ahead) { return t + 1 < ahead ? 1 : 2; }              // from K_t to K_{t+1}
+__device__ __forceinline__ int step_of_values(int t, int n, int ahead) { return t + ahead < n ? 2 : 1; }     // from V_t to V_{t+1}
 
 // bits 0..31: columns c < n
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
@@ -293,6 +288,30 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// x, y = x * unit + shift, y * unit + shift and a, b += x, y, two in one instruction
+__device__ __forceinline__ void scale_add2(float &x, float &y, float unit, float shift) {
+  asm("{\n\t.reg .b64 v, u, s;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 u, {%2, %2};\n\tmov.b64 s, {%3, %3};\n\tfma.rn.f32x2 v, v, u, s;\n\tmov.b64 {%0, %1}, v;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(unit), "f"(shift));
+}
+__device__ __forceinline__ void add2(float &a, float &b, float x, float y) {
+  asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\tadd.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
+// the maximum of row r over the accumulators and the row's copies
+__device__ __forceinline__ float row_maximum(const float2 (*ml)[kRows], int r, int copy_rows) {
+  float m = -INFINITY;
+  for (int i = r; i < kRows; i += copy_rows) m = fmaxf(m, fmaxf(ml[0][i].x, ml[1][i].x));
+  return m;
+}
+
+// logits whose bit (from `first` on) is not set become -inf
+__device__ __forceinline__ void mask16(bool masked, uint32_t on, int first, uint32_t *y) {
+  if (!masked) return;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) y[j] = on >> (first + j) & 1 ? y[j] : 0xFF800000u;
+}
+
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
   const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
@@ -303,10 +322,116 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
   return *reinterpret_cast<const uint32_t *>(&x);
 }
 
+// A row's softmax over 16 * kChunks of a tile's logits, from column `first` on.  16 logits at a time.  Once a row has a maximum the weights are
+// computed with it at once, and their own maximum is taken on the way: it hardly ever asks for another one.
+template <typename T, int D, int kChunks>
+__device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int first, bool masked, const uint32_t *on, float unit, bool has_sums, float &m,
+                                             float &l) {
+  uint32_t r[2][16], packed[8 * kChunks];
+  const uint32_t from = my_s + first;
+  bool known = __any_sync(~0u, m == -INFINITY), again = known;
+  float sum[4];
+  for (;;) {
+    if (again) {
+      float top[2] = {-INFINITY, -INFINITY};
+      tmem_load16(from, r[0]);
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        tmem_wait_loads();
+        if (i + 1 < kChunks) tmem_load16(from + 16 * (i + 1), r[(i + 1) & 1]);
+        mask16(masked, on[i >> 1], (i & 1) * 16, r[i & 1]);
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) top[(j >> 1) & 1] = fmaxf(fmaxf(top[(j >> 1) & 1], __uint_as_float(r[i & 1][j])), __uint_as_float(r[i & 1][j + 1]));
+      }
+      const float highest = fmaxf(top[0], top[1]);
+      // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
+      const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
+      const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
+      if (raise) { l *= factor; m = highest; }
+      if (__any_sync(~0u, raise) && has_sums) {
+#pragma unroll 1
+        for (int i = 0; i < D; i += 16) {
+          tmem_load16(my_o + i, r[0]);
+          tmem_wait_loads();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) r[0][j] = __float_as_uint(__uint_as_float(r[0][j]) * factor);
+          tmem_store16(my_o + i, r[0]);
+        }
+      }
+    }
+    const float shift = m == -INFINITY ? 0.f : -m * unit;
+    float top[2] = {-INFINITY, -INFINITY};
+    sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+    tmem_load16(from, r[0]);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      tmem_wait_loads();
+      if (i + 1 < kChunks) tmem_load16(from + 16 * (i + 1), r[(i + 1) & 1]);
+      uint32_t *y = r[i & 1];
+      mask16(masked, on[i >> 1], (i & 1) * 16, y);
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        float a = __uint_as_float(y[j]), b = __uint_as_float(y[j + 1]), c = __uint_as_float(y[j + 2]), d = __uint_as_float(y[j + 3]);
+        top[0] = fmaxf(fmaxf(top[0], a), b);
+        top[1] = fmaxf(fmaxf(top[1], c), d);
+        scale_add2(a, b, unit, shift);
+        scale_add2(c, d, unit, shift);
+        a = exp2_fast(a); b = exp2_fast(b); c = exp2_fast(c); d = exp2_fast(d);
+        add2(sum[0], sum[1], a, b);
+        add2(sum[2], sum[3], c, d);
+        packed[8 * i + j / 2] = pack<T>(a, b);
+        packed[8 * i + j / 2 + 1] = pack<T>(c, d);
+      }
+    }
+    if (known) break;
+    known = again = __any_sync(~0u, (fmaxf(top[0], top[1]) - m) * unit > kRaise);
+    if (!again) break;
+  }
+  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+  for (int i = 0; i < kChunks; i += 2) tmem_store16(my_s + first / 2 + 8 * i, packed + 8 * i);
+  if (kChunks < 8) {                        // the keys of the other copies
+    uint32_t zero[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+      if (i * 16 < first || i * 16 >= first + kChunks * 16) tmem_store16(my_s + 8 * i, zero);
+  }
+}
+
+// The block's rows [0, rows) of queries, `copies` times, swizzled; 256 threads.  All loads go out before `ready` is asked for, which says that the memory is free.
+template <typename T, int D, typename Ready>
+__device__ __forceinline__ bool load_queries(const Params &p, const Block &w, unsigned char *q, int copy_rows, Ready ready) {
+  constexpr int kPieces = D / 8, kPass = kSoftmaxThreads / kPieces, kPasses = kRows / kPass;       // 16 (32) rows a pass
+  const int piece = threadIdx.x % kPieces, row = threadIdx.x / kPieces;
+  const T *from = static_cast<const T *>(p.a.q_dev) + w.b * p.a.q_seq_stride + piece * 8;
+  uint4 x[kPasses];
+#pragma unroll 1
+  for (int half = 0; half < (w.rows > kRows ? 2 : 1); ++half) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int r = half * kRows + ((row + i * kPass) & (copy_rows - 1));
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (r < w.rows) {
+        const int at = w.row0 + r, node = token_of(p, at), h = w.head * p.group + at - node * p.group;
+        x[i] = *reinterpret_cast<const uint4 *>(from + node * p.a.q_token_stride + h * p.a.q_head_stride);
+      }
+    }
+    if (half == 0 && !ready()) return false;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int place = row + i * kPass;
+      *reinterpret_cast<uint4 *>(q + half * (kRows * D * 2) + (piece >> 3) * (kRows * 128) + place * 128 + (((piece & 7) ^ (place & 7)) << 4)) = x[i];
+    }
+  }
+  return true;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
   constexpr int kRing = Ring<D>::n;
-  constexpr bool kBf16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ __align__(1024) unsigned char raw[];       // (the tiles' swizzle goes by the address)
   Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -317,60 +442,89 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { barrier_init(sh.full + i, 1); barrier_init(sh.empty + i, 1); }
     for (int s = 0; s < 2; ++s) { barrier_init(sh.logits + s, 1); barrier_init(sh.weights + s, kRows); }
+    for (int i = 0; i < kBlocks; ++i) { barrier_init(sh.described + i, 1); barrier_init(sh.read + i, kReaders); }
     barrier_init(&sh.done, 1);
     barrier_init(&sh.queries, kSoftmaxThreads);
-    barrier_init(&sh.halves, kSoftmaxThreads);
+    barrier_init(&sh.meet, kSoftmaxThreads);
     barrier_init_fence();
     sh.gave_up = 0;
+    sh.left = 0;
     tensor_map_prefetch(&maps.k);
     tensor_map_prefetch(&maps.v);
   }
   chain_wait();
 
-  // ---- the block's share of the tiles
+  // ---- the thread block's share of the tiles
   if (p.split) {
     long long carry = 0;
-    for (int base = 0; base < n_pairs; base += kThreads) {
-      const int pair = base + tid;
-      const long long mine = pair < n_pairs ? block_of(p, pair).tiles : 0;
-      long long x = mine;
+    if (n_pairs <= kThreads) {              // everything in one round: no need for the list
+      const Block w = tid < n_pairs ? block_of(p, tid) : Block{};
+      long long x = tid < n_pairs ? w.tiles : 0;
+      const int mine = (int)x;
       for (int d = 1; d < 32; d <<= 1) {
         const long long y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
       }
       if (lane == 31) sh.warp_sum[warp] = x;
       __syncthreads();
-      long long earlier = 0, all = 0;
-      for (int w = 0; w < kThreads / 32; ++w) {
-        const long long s = sh.warp_sum[w];
-        earlier += w < warp ? s : 0;
-        all += s;
+      long long earlier = 0;
+      for (int v = 0; v < kThreads / 32; ++v) {
+        const long long s = sh.warp_sum[v];
+        earlier += v < warp ? s : 0;
+        carry += s;
       }
-      if (pair < n_pairs) sh.before[pair] = carry + earlier + x - mine;
-      carry += all;
+      const Deal deal(carry * p.c.kv_heads, G);
+      const long long begin = deal.begin(blockIdx.x), first = (earlier + x - mine) * p.c.kv_heads;
+      if (tid == 0) sh.left = deal.begin(blockIdx.x + 1) - begin;
+      if (mine > 0 && begin >= first && begin < first + (long long)mine * p.c.kv_heads) {
+        const long long in_pair = begin - first;
+        sh.pair = tid;
+        sh.head = (int)(in_pair < 0x7FFFFFFF ? (uint32_t)in_pair / (uint32_t)mine : in_pair / mine);
+        sh.k0 = (int)(in_pair - (long long)sh.head * mine);
+      }
+    } else {
+      for (int base = 0; base < n_pairs; base += kThreads) {
+        const int pair = base + tid;
+        const long long mine = pair < n_pairs ? block_of(p, pair).tiles : 0;
+        long long x = mine;
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long y = __shfl_up_sync(~0u, x, d);
+          if (lane >= d) x += y;
+        }
+        if (lane == 31) sh.warp_sum[warp] = x;
+        __syncthreads();
+        long long earlier = 0, all = 0;
+        for (int v = 0; v < kThreads / 32; ++v) {
+          const long long s = sh.warp_sum[v];
+          earlier += v < warp ? s : 0;
+          all += s;
+        }
+        if (pair < n_pairs) sh.before[pair] = carry + earlier + x - mine;
+        carry += all;
+        __syncthreads();
+      }
+      if (tid == 0) sh.before[n_pairs] = carry;
       __syncthreads();
+      const Deal deal(carry * p.c.kv_heads, G);
+      const long long begin = deal.begin(blockIdx.x);
+      if (tid == 0) sh.left = deal.begin(blockIdx.x + 1) - begin;
+      for (int pair = tid; pair < n_pairs; pair += kThreads) {
+        const long long first = sh.before[pair] * p.c.kv_heads, last = sh.before[pair + 1] * p.c.kv_heads;
+        if (begin < first || begin >= last) continue;
+        const long long mine = sh.before[pair + 1] - sh.before[pair], in_pair = begin - first;
+        sh.pair = pair;
+        sh.head = (int)(in_pair / mine);
+        sh.k0 = (int)(in_pair % mine);
+      }
     }
+    __syncthreads();
     if (tid == 0) {
-      const long long total = carry * p.c.kv_heads, used = total < G ? max(total, 1ll) : G;        // (no block without a tile)
-      const long long begin = blockIdx.x < used ? blockIdx.x * total / used : total, end = blockIdx.x < used ? (blockIdx.x + 1) * total / used : total;
-      sh.left = end - begin;
       int4 cut = make_int4(-1, 0, 0, 0);
-      if (end > begin) {
-        int lo = 0, hi = n_pairs;           // the last pair whose tiles begin at or before `begin` and that has any
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (sh.before[mid] * p.c.kv_heads <= begin) lo = mid; else hi = mid;
-        }
-        const long long tiles = (lo + 1 < n_pairs ? sh.before[lo + 1] : carry) - sh.before[lo];
-        const long long in_pair = begin - sh.before[lo] * p.c.kv_heads;
-        sh.pair = lo;
-        sh.head = (int)(in_pair / tiles);
-        sh.k0 = (int)(in_pair % tiles);
-        if (sh.k0 > 0) {                    // a block of rows that an earlier thread block began
-          const long long item = begin - sh.k0, item_last = item + tiles - 1;
-          const int c0 = (int)(((item + 1) * used - 1) / total), c1 = (int)(((item_last + 1) * used - 1) / total);
-          if (c0 == (int)blockIdx.x - 1) cut = make_int4(lo, sh.head, c0, c1);
-        }
+      if (sh.left > 0 && sh.k0 > 0) {       // a block of rows that an earlier thread block began
+        const Deal deal(carry * p.c.kv_heads, G);
+        const long long item = deal.begin(blockIdx.x) - sh.k0, last = item + block_of(p, sh.pair).tiles - 1;
+        const int c0 = deal.owner(item);
+        if (c0 == (int)blockIdx.x - 1) cut = make_int4(sh.pair, sh.head, c0, deal.owner(last));
       }
       p.cut[blockIdx.x] = cut;
     }
@@ -379,348 +533,419 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = sh.tmem;
-  Walk x;
-  x.left = sh.left;
-  x.pair = sh.pair; x.head = sh.head; x.k0 = sh.k0; x.k1 = 0;
-  __syncthreads();                          // (the ring's memory is free from here on)
-  bool more = p.split ? x.left > 0 : true;
-  if (p.split && more) x.w = block_of(p, x.pair);
-  more = more && walk_next(p, x, n_pairs, true);
 
-  if (warp == 9) {
-    // ------------------------------------------------------------ copies
-    const int box_bytes = p.box_rows * 128, boxes = kTile / p.box_rows * (D / 64);
-    const int half = lane / (kTile / p.box_rows), part = lane % (kTile / p.box_rows);
-    const int page_shift = __ffs(p.c.page_size) - 1;
-    int turn = 0;                           // buffers filled so far
-    bool ok = true;
-    for (; more && ok; more = walk_next(p, x, n_pairs, false)) {
-      const Block &w = x.w;
-      const int n = x.k1 - x.k0, ahead = w.rows > kRows ? 1 : 2;
-      if (x.head == 0 && x.k0 == 0 && w.row0 == 0 && lane == 0 && w.see.keys < w.see.prefix + w.see.n) cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
-      const int32_t *table = p.c.table_dev + (long long)w.b * p.c.max_pages;
-      for (int i = 0; i < 2 * n && ok; ++i, ++turn) {
-        // the i-th copy of the walk's order: keys or values of which tile
-        const bool values = i < min(n, ahead) ? false : i >= 2 * n - min(n, ahead) ? true : ((i - ahead) & 1) == 0;
-        const int t = !values ? (i < ahead ? i : (i + ahead - 1) / 2) : i >= 2 * n - min(n, ahead) ? i - n : (i - ahead) / 2;
-        const int key = w.key0(x.k0 + t) + part * p.box_rows;
-        int page = p.c.n_pages;             // behind the pool: zeros
-        if (lane < boxes && key < w.see.keys) {
-          page = table[key >> page_shift];
-          if (page < 0 || page >= p.c.n_pages) {
-            page = p.c.n_pages;
-            cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
+  // the i-th block of rows of the share; rows = 0 behind the last
+  auto described = [&](int i) { return wait(sh, sh.described + i % kBlocks, i / kBlocks & 1); };
+  auto block_read = [&](int i) {
+    __syncwarp();
+    if (lane == 0) barrier_arrive(sh.read + i % kBlocks);
+  };
+
+  if (warp == 10) {
+    // ------------------------------------------------------------ the walk
+    if (lane == 0) {
+      long long left = sh.left, item = blockIdx.x;
+      int pair = sh.pair, head = sh.head, k0 = sh.k0, known = -1;
+      Block w;
+      w.rows = 0;
+      for (int i = 0;; ++i) {
+        bool more = false;
+        if (p.split) {
+          while (left > 0 && pair < n_pairs) {
+            if (pair != known) { w = block_of(p, pair); known = pair; }
+            if (w.tiles > 0) { more = true; break; }
+            ++pair;
+          }
+          if (more) {
+            w.head = head;
+            w.k0 = k0;
+            w.k1 = (int)min((long long)w.tiles, k0 + left);
+            left -= w.k1 - k0;
+            k0 = 0;
+            if (++head == p.c.kv_heads) { head = 0; ++pair; }
+          }
+        } else {
+          for (; item < (long long)n_pairs * p.c.kv_heads && !more; item += G) {
+            pair = (int)(item / p.c.kv_heads);
+            if (pair != known) { w = block_of(p, pair); known = pair; }
+            w.head = (int)(item - (long long)pair * p.c.kv_heads);
+            w.k1 = w.tiles;
+            more = w.tiles > 0;
           }
         }
-        const int at = turn % kRing;
-        ok = wait(sh, sh.empty + at, (turn / kRing & 1) ^ 1);
-        ok = __all_sync(~0u, ok);
+        if (!wait(sh, sh.read + i % kBlocks, (i / kBlocks & 1) ^ 1)) break;
+        if (!more) w.rows = 0;
+        sh.block[i % kBlocks] = w;
+        barrier_arrive(sh.described + i % kBlocks);
+        if (!more) break;
+      }
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ copies
+    const int parts = kTile / p.box_rows, box_bytes = p.box_rows * 128, boxes = parts * (D / 64);
+    const int half = lane / parts, part = lane % parts, page_shift = __ffs(p.c.page_size) - 1;
+    Cursor<kRing> to = {0, 0};
+    int filled = 0;
+    bool ok = true;
+    for (int item = 0;; ++item) {
+      if (!(ok = __all_sync(~0u, described(item)))) break;
+      const Block w = sh.block[item % kBlocks];
+      block_read(item);
+      if (w.rows == 0) break;
+      const int n = w.k1 - w.k0, ahead = w.rows > kRows ? 1 : 2, lead = min(n, ahead);
+      if (w.head == 0 && w.k0 == 0 && w.row0 == 0 && lane == 0 && w.keys < w.prefix + w.n) cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
+      const int32_t *table = p.c.table_dev + (long long)w.b * p.c.max_pages;
+      // the next copy of the order and the page that this lane copies for it (behind the pool: zeros)
+      auto page_of = [&](int i, bool &values, int &key) {
+        values = i >= lead && (i >= 2 * n - lead || ((i - ahead) & 1) == 0);
+        const int t = values ? (i >= 2 * n - lead ? i - n : (i - ahead) >> 1) : (i < ahead ? i : (i + ahead - 1) >> 1);
+        key = w.key0(w.k0 + t) + part * p.box_rows;
+        if (i >= 2 * n || lane >= boxes || key >= w.keys) return p.c.n_pages;
+        return (int)table[key >> page_shift];
+      };
+      bool values, next_values;
+      int key, next_key, page = page_of(0, values, key);
+      for (int i = 0; i < 2 * n; ++i) {
+        const int next = page_of(i + 1, next_values, next_key);
+        ok = __all_sync(~0u, wait(sh, sh.empty + to.at, to.parity ^ 1));
         if (!ok) break;
-        if (lane == 0) barrier_expect(sh.full + at, Ring<D>::bytes);
+        if (lane == 0) barrier_expect(sh.full + to.at, Ring<D>::bytes);
+        if (page < 0 || page > p.c.n_pages || (page == p.c.n_pages && key < w.keys && lane < boxes)) {
+          page = p.c.n_pages;
+          cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
+        }
         __syncwarp();
         if (lane < boxes)
-          copy_box(shared_address(sh.ring[at]) + half * (kTile * 128) + part * box_bytes, values ? &maps.v : &maps.k, sh.full + at, half * 64, x.head,
+          copy_box(shared_address(sh.ring[to.at]) + half * (kTile * 128) + part * box_bytes, values ? &maps.v : &maps.k, sh.full + to.at, half * 64, w.head,
                    key & (p.c.page_size - 1), page, p.a.layer);
+        to.step(1);
+        ++filled;
+        page = next; values = next_values; key = next_key;
       }
-      if (!ok && lane == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
+      if (!ok) {
+        if (lane == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
+        break;
+      }
     }
-    if (*(volatile int *)&sh.gave_up && lane == 0)             // nothing may arrive in a block's memory that has ended
-      for (int i = max(turn - kRing, 0); i < turn; ++i)
+    if (!ok && lane == 0)                   // nothing may arrive in a block's memory that has ended
+      for (int i = max(filled - kRing, 0); i < filled; ++i)
         for (int tries = 0; tries < kTries && !barrier_try(sh.full + i % kRing, i / kRing & 1); ++tries) {}
     __syncwarp();
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
-    if (lane == 0) {
-      constexpr uint32_t kLogits = product_descriptor(kBf16, kTile, false), kMix = product_descriptor(kBf16, D, true);
-      const uint32_t q0 = shared_address(sh.q[0]), q1 = shared_address(sh.q[1]);
-      int turn = 0, items = 0, weights_turn[2] = {0, 0};
-      bool ok = true;
-      auto buffer = [&](int i) { return shared_address(sh.ring[(turn + i) % kRing]); };
-      auto filled = [&](int i) { return wait(sh, sh.full + (turn + i) % kRing, (turn + i) / kRing & 1); };
-      auto release = [&](int i) { products_commit(sh.empty + (turn + i) % kRing); };
-      auto logits = [&](int s, uint32_t q, uint32_t k) {
+    // The whole warp goes along, so that what the instructions take lies in uniform registers; one lane issues them.
+    constexpr uint32_t kLogits = product_descriptor(kBf16, kTile, false), kMix = product_descriptor(kBf16, D, true);
+    const uint64_t q_tile = tile_descriptor(shared_address(sh.q[0]), 1024, 16), k_tile = tile_descriptor(shared_address(sh.ring[0]), 1024, 16),
+                   v_tile = tile_descriptor(shared_address(sh.ring[0]), 1024, kTile * 128);
+    const bool leader = elect_one();
+    Cursor<kRing> keys = {0, 0}, vals;
+    uint32_t weights_parity[2] = {0, 0};
+    bool ok = true;
+    int item = 0;
+    auto arrived = [&](uint64_t *bar, uint32_t parity) { return __all_sync(~0u, wait(sh, bar, parity)) != 0; };
+    auto logits = [&](int s, int half, int buffer) {
+      const uint64_t a = q_tile + half * (kRows * D * 2 / 16), b = k_tile + (uint32_t)buffer * (Ring<D>::bytes / 16);
+      if (leader) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          const uint32_t off = (d >> 2) * (kTile * 128) + (d & 3) * 32;         // 64 elements, then the other 64; 16 of them a step
-          product_shared(tmem + s * kTile, tile_descriptor(q + off, 1024, 16), tile_descriptor(k + off, 1024, 16), kLogits, d > 0);
+        for (int d = 0; d < D / 16; ++d) {                      // 64 elements, then the other 64; 16 of them a step
+          const int off = ((d >> 2) * (kTile * 128) + (d & 3) * 32) / 16;
+          product_shared(tmem + s * kTile, a + off, b + off, kLogits, d > 0);
         }
         products_commit(sh.logits + s);
-      };
-      auto mix = [&](int s, uint32_t v, bool add) {
-        ok = ok && wait(sh, sh.weights + s, weights_turn[s]++ & 1);
-        if (!ok) return;
-        tmem_fence_after();
+      }
+      __syncwarp();
+    };
+    auto mix = [&](int s, int buffer, bool add) {
+      const uint64_t b = v_tile + (uint32_t)buffer * (Ring<D>::bytes / 16);
+      if (leader) {
 #pragma unroll
         for (int d = 0; d < kTile / 16; ++d)
-          product_tensor(tmem + 256 + s * 128, tmem + s * kTile + d * 8, tile_descriptor(v + d * 2048, 1024, kTile * 128), kMix, add || d > 0);
-      };
-      for (; more && ok; more = walk_next(p, x, n_pairs, false), ++items) {
-        const int n = x.k1 - x.k0;
-        ok = wait(sh, &sh.queries, items & 1);
-        if (!ok) break;
-        tmem_fence_after();
-        if (x.w.rows > kRows) {             // both halves of the rows over every tile
-          if (!(ok = filled(0))) break;
-          logits(0, q0, buffer(0));
-          logits(1, q1, buffer(0));
-          release(0);
-          for (int t = 0; t < n && ok; ++t) {
-            const int v = place_of_values(t, n, 1), k = place_of_keys(t + 1, 1);
-            if (!(ok = filled(v))) break;
-            mix(0, buffer(v), t > 0);
-            if (!ok) break;
-            if (t + 1 < n) {
-              if (!(ok = filled(k))) break;
-              logits(0, q0, buffer(k));
-            }
-            mix(1, buffer(v), t > 0);
-            if (!ok) break;
-            release(v);
-            if (t + 1 < n) {
-              logits(1, q1, buffer(k));
-              release(k);
-            }
+          product_tensor(tmem + 256 + s * 128, tmem + s * kTile + d * 8, b + d * (2048 / 16), kMix, add || d > 0);
+      }
+      __syncwarp();
+    };
+    auto free_buffer = [&](int buffer) {
+      if (leader) products_commit(sh.empty + buffer);
+      __syncwarp();
+    };
+    for (;; ++item) {
+      if (!(ok = arrived(sh.described + item % kBlocks, item / kBlocks & 1))) break;
+      const int n = uniform(sh.block[item % kBlocks].k1 - sh.block[item % kBlocks].k0), rows = uniform(sh.block[item % kBlocks].rows);
+      block_read(item);
+      if (rows == 0) break;
+      const int ahead = rows > kRows ? 1 : 2;
+      vals = keys;
+      vals.step(min(n, ahead));
+      if (!(ok = arrived(&sh.queries, item & 1))) break;
+      tmem_fence_after();
+      if (rows > kRows) {                   // both halves of the rows over every tile
+        if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
+        logits(0, 0, keys.at);
+        logits(1, 1, keys.at);
+        free_buffer(keys.at);
+        for (int t = 0; t < n; ++t) {
+          keys.step(2);
+          if (!(ok = arrived(sh.full + vals.at, vals.parity))) break;
+          if (!(ok = arrived(sh.weights, weights_parity[0]))) break;
+          weights_parity[0] ^= 1;
+          tmem_fence_after();
+          mix(0, vals.at, t > 0);
+          if (t + 1 < n) {
+            if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
+            logits(0, 0, keys.at);
           }
-        } else {                            // all rows, every other tile
-          for (int t = 0; t < min(n, 2) && ok; ++t) {
-            if (!(ok = filled(t))) break;
-            logits(t, q0, buffer(t));
-            release(t);
+          if (!(ok = arrived(sh.weights + 1, weights_parity[1]))) break;
+          weights_parity[1] ^= 1;
+          tmem_fence_after();
+          mix(1, vals.at, t > 0);
+          free_buffer(vals.at);
+          if (t + 1 < n) {
+            logits(1, 1, keys.at);
+            free_buffer(keys.at);
           }
-          for (int t = 0; t < n && ok; ++t) {
-            const int v = place_of_values(t, n, 2), k = place_of_keys(t + 2, 2);
-            if (!(ok = filled(v))) break;
-            mix(t & 1, buffer(v), t > 1);
-            if (!ok) break;
-            release(v);
-            if (t + 2 < n) {
-              if (!(ok = filled(k))) break;
-              logits(t & 1, q0, buffer(k));
-              release(k);
-            }
-          }
+          vals.step(step_of_values(t, n, 1));
         }
-        if (!ok) break;
-        products_commit(&sh.done);
-        turn += 2 * n;
+      } else {                              // all rows, every other tile
+        for (int t = 0; t < min(n, 2); ++t) {
+          if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
+          logits(t, 0, keys.at);
+          free_buffer(keys.at);
+          keys.step(step_of_keys(t, 2));
+        }
+        for (int t = 0; t < n && ok; ++t) {
+          const int s = t & 1;
+          if (!(ok = arrived(sh.full + vals.at, vals.parity))) break;
+          if (!(ok = arrived(sh.weights + s, s ? weights_parity[1] : weights_parity[0]))) break;
+          if (s) weights_parity[1] ^= 1; else weights_parity[0] ^= 1;
+          tmem_fence_after();
+          mix(s, vals.at, t > 1);
+          free_buffer(vals.at);
+          if (t + 2 < n) {
+            if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
+            logits(s, 0, keys.at);
+            free_buffer(keys.at);
+            keys.step(2);
+          }
+          vals.step(step_of_values(t, n, 2));
+        }
       }
-      if (!ok) {                            // what is in flight must not outlive its tensor memory
-        products_commit(&sh.done);
-        for (int tries = 0; tries < kTries && !barrier_try(&sh.done, items & 1); ++tries) {}
-      }
+      if (!ok) break;
+      if (leader) products_commit(&sh.done);
+      __syncwarp();
+      keys = vals;
+    }
+    if (!ok && leader) {                    // what is in flight must not outlive its tensor memory
+      products_commit(&sh.done);
+      for (int tries = 0; tries < kTries && !barrier_try(&sh.done, item & 1); ++tries) {}
     }
     __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax
     const int s = warp >> 2, row = tid & 127;                   // the accumulator; the row in it = the lane of tensor memory
-    const uint32_t my_s = tmem + s * kTile + ((uint32_t)(warp & 3) << 21), my_o = my_s + 256 + s * (128 - kTile);
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, my_s = tmem + s * kTile + lanes, my_o = tmem + 256 + s * 128 + lanes;
     const float unit = p.a.scale * kLog2e;
-    int turn = 0, items = 0, logits_turn = 0, both_turn = 0;
+    float *stage = reinterpret_cast<float *>(sh.q[0]) + warp * (D * 16);        // D * 64 bytes a warp
+    Cursor<kRing> vals_at, base = {0, 0};
+    uint32_t logits_parity = 0, meet_parity = 0;
     bool ok = true;
-    for (; more && ok; more = walk_next(p, x, n_pairs, false), ++items) {
-      const Block &w = x.w;
-      const Sight &see = w.see;
+    int item = 0, turn = 0;                 // buffers of the ring so far
+    auto all_meet = [&] {
+      barrier_arrive(&sh.meet);
+      const bool met = wait(sh, &sh.meet, meet_parity);
+      meet_parity ^= 1;
+      return met;
+    };
+    for (;; ++item) {
+      if (!(ok = described(item))) break;
+      const Block &w = sh.block[item % kBlocks];
+      if (w.rows == 0) break;
       const bool two = w.rows > kRows;
-      const int n = x.k1 - x.k0, ahead = two ? 1 : 2;
-      // the rows' queries, swizzled
-      {
-        constexpr int kPieces = D / 8;
-        const int halves = two ? 2 : 1;
-        for (int i = tid; i < halves * kRows * kPieces; i += kSoftmaxThreads) {
-          const int r = i / kPieces, piece = i % kPieces, place = r & 127;
-          uint4 q = make_uint4(0, 0, 0, 0);
-          if (r < w.rows) {
-            const int at = w.row0 + r, node = at / p.group, h = x.head * p.group + at - node * p.group;
-            q = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.a.q_dev) + w.b * p.a.q_seq_stride + node * p.a.q_token_stride +
-                                                 h * p.a.q_head_stride + piece * 8);
-          }
-          *reinterpret_cast<uint4 *>(sh.q[r >> 7] + (piece >> 3) * (kRows * 128) + place * 128 + (((piece & 7) ^ (place & 7)) << 4)) = q;
-        }
-        shared_writes_fence();
-        tmem_fence_before();
-        barrier_arrive(&sh.queries);
-      }
-      const int my_row = two ? s * kRows + row : row;            // in the block
+      const int copy_rows = w.rows <= 32 ? 32 : w.rows <= 64 ? 64 : kRows;      // rows of a copy
+      const int n = w.k1 - w.k0, ahead = two ? 1 : 2;
+      ok = load_queries<T, D>(p, w, sh.q[0], copy_rows, [&] { return item == 0 || all_meet(); });       // (no sums of the last block in there any more)
+      if (!ok) break;
+      shared_writes_fence();
+      tmem_fence_before();
+      barrier_arrive(&sh.queries);
+
+      const int my_row = two ? s * kRows + row : row & (copy_rows - 1);         // in the block
+      const int first_column = row & ~(copy_rows - 1);                          // of a copy's keys: as many as it has rows
       const bool live = my_row < w.rows;
       const bool warp_live = (my_row & ~31) < w.rows;
-      const int at = w.row0 + (live ? my_row : w.rows - 1), node = at / p.group, head = x.head * p.group + at - node * p.group;
-      const int own = see.position(node);
+      const int node = token_of(p, w.row0 + (live ? my_row : w.rows - 1));
       float m = -INFINITY, l = 0.f;
-      for (int t = two ? 0 : s; t < n; t += ahead) {
-        const int key = w.key0(x.k0 + t);
-        const bool all = key + kTile <= see.prefix && key + kTile <= see.keys && (see.window == 0 || key > own - see.window || key + kTile <= see.sinks);
-        const bool masked = !__all_sync(~0u, all);
-        uint32_t on0 = ~0u, on1 = ~0u, on2 = ~0u, on3 = ~0u;
-        if (masked && warp_live) {          // (while the logits are on their way)
+      {
+        const Sight see = sight_of(p, w);
+        const int own = see.position(node);
+        vals_at = base;
+        vals_at.step(min(n, ahead));
+        if (!two && s == 1) vals_at.step(step_of_values(0, n, ahead));
+        for (int t = two ? 0 : s; t < n; t += ahead) {
+          const int key = w.key0(w.k0 + t);
+          const bool all = key + kTile <= see.prefix && key + kTile <= see.keys && (see.window == 0 || key > own - see.window || key + kTile <= see.sinks);
+          const bool masked = !__all_sync(~0u, all);
+          uint32_t on[4] = {~0u, ~0u, ~0u, ~0u};
+          if (masked && warp_live) {        // (while the logits are on their way)
 #pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            on0 = on1; on1 = on2; on2 = on3;
-            on3 = sight_bits(see, node, own, key + 32 * i);
+            for (int i = copy_rows / 32; i > 0; --i) {
+              on[3] = on[2]; on[2] = on[1]; on[1] = on[0];
+              on[0] = sight_bits(see, node, own, key + first_column + 32 * (i - 1));
+            }
           }
+          if (!(ok = wait(sh, sh.logits + s, logits_parity))) break;
+          logits_parity ^= 1;
+          tmem_fence_after();
+          if (key + kTile > see.keys) {     // rows of the values that nobody wrote: their weights are 0, they must be numbers
+            if (!(ok = wait(sh, sh.full + vals_at.at, vals_at.parity))) break;
+            if (key + row >= see.keys && !(two && s == 1)) {    // (the first group's are in time for both)
+#pragma unroll
+              for (int i = 0; i < D / 8; ++i)
+                *reinterpret_cast<uint4 *>(sh.ring[vals_at.at] + (i >> 3) * (kTile * 128) + row * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            shared_writes_fence();
+          }
+          vals_at.step(step_of_values(t, n, ahead));
+          if (!two) vals_at.step(step_of_values(t + 1, n, ahead));
+          __syncwarp();
+          if (warp_live) {
+            if (copy_rows == 32) softmax_tile<T, D, 2>(my_s, my_o, first_column, masked, on, unit, t >= ahead, m, l);
+            else if (copy_rows == 64) softmax_tile<T, D, 4>(my_s, my_o, first_column, masked, on, unit, t >= ahead, m, l);
+            else softmax_tile<T, D, 8>(my_s, my_o, 0, masked, on, unit, t >= ahead, m, l);
+            tmem_wait_stores();
+          }
+          tmem_fence_before();
+          barrier_arrive(sh.weights + s);
         }
-        if (!(ok = wait(sh, sh.logits + s, logits_turn++ & 1))) break;
-        tmem_fence_after();
-        if (key + kTile > see.keys) {       // rows of the values that nobody wrote: their weights are 0, they must be numbers
-          const int at_v = turn + place_of_values(t, n, ahead);
-          if (!(ok = wait(sh, sh.full + at_v % kRing, at_v / kRing & 1))) break;
-          if (key + row >= see.keys && !(two && s == 1)) {       // (the first group's are in time for both)
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-              *reinterpret_cast<uint4 *>(sh.ring[at_v % kRing] + (i >> 3) * (kTile * 128) + row * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-          }
-          shared_writes_fence();
-        }
-        __syncwarp();
-        if (warp_live) {
-          // 32 logits at a time, and once more for the weights: to read tensor memory twice is cheaper than 128 registers
-          uint32_t r[2][32];
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          tmem_load32(my_s, r[0]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            tmem_wait_loads();
-            if (i < 3) tmem_load32(my_s + 32 * (i + 1), r[(i + 1) & 1]);
-            const uint32_t on = i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3;
-            uint32_t *y = r[i & 1];
-            if (masked) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = on >> j & 1 ? y[j] : 0xFF800000u;
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(y[j]));
-          }
-          tmem_load32(my_s, r[0]);
-          const float highest = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-          // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
-          const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
-          const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
-          if (raise) { l *= factor; m = highest; }
-          if (__any_sync(~0u, raise) && t >= ahead) {
-#pragma unroll
-            for (int i = 0; i < D; i += 16) {
-              uint32_t o[16];
-              tmem_load16(my_o + i, o);
-              tmem_wait_loads();
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
-              tmem_store16(my_o + i, o);
-            }
-          }
-          const float shift = m == -INFINITY ? 0.f : m * unit;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            tmem_wait_loads();
-            if (i < 3) tmem_load32(my_s + 32 * (i + 1), r[(i + 1) & 1]);
-            const uint32_t on = i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3;
-            uint32_t *y = r[i & 1];
-            if (masked) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = on >> j & 1 ? y[j] : 0xFF800000u;
-            }
-            uint32_t packed[16];
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float lo = exp2_fast(fmaf(__uint_as_float(y[j]), unit, -shift)), hi = exp2_fast(fmaf(__uint_as_float(y[j + 1]), unit, -shift));
-              sum[j & 2] += lo;
-              sum[(j & 2) + 1] += hi;
-              packed[j / 2] = pack<T>(lo, hi);
-            }
-            tmem_store16(my_s + 16 * i, packed);                // over logits that have been read
-          }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          tmem_wait_stores();
-        }
-        tmem_fence_before();
-        barrier_arrive(sh.weights + s);
       }
-      if (!ok || !(ok = wait(sh, &sh.done, items & 1))) {
+      if (!ok || !(ok = wait(sh, &sh.done, item & 1))) {
         if (tid == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
-        ok = false;
         break;
       }
       tmem_fence_after();
       turn += 2 * n;
+      base.at = turn % kRing;
+      base.parity = turn / kRing & 1;
 
-      // what the block has of its rows: finished, or a part for the other launch to add up
+      // ---- what the thread block has of its rows: finished, or a part for the other launch to add up
+      const bool whole = w.k0 == 0 && w.k1 == w.tiles;
       m = m == -INFINITY ? m : m * unit;
       float factor0 = 1.f, factor1 = 0.f;
-      int column0 = 0, columns = D;
-      if (!two) {
+      if (!two) {                           // over the two accumulators and the copies of the row
         sh.ml[s][row] = make_float2(m, l);
-        barrier_arrive(&sh.halves);
-        if (!(ok = wait(sh, &sh.halves, both_turn++ & 1))) {
-          if (tid == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
-          break;
-        }
-        const float2 e = sh.ml[0][row], o = sh.ml[1][row];          // (written again only after all threads' next queries)
-        m = fmaxf(e.x, o.x);
-        factor0 = e.x == -INFINITY ? 0.f : exp2_fast(e.x - m);
-        factor1 = o.x == -INFINITY ? 0.f : exp2_fast(o.x - m);
-        l = e.y * factor0 + o.y * factor1;
-        columns = D / 2;
-        column0 = s * columns;
+        if (!(ok = all_meet())) break;
+        m = -INFINITY;
+        for (int i = my_row; i < kRows; i += copy_rows) m = fmaxf(m, fmaxf(sh.ml[0][i].x, sh.ml[1][i].x));
+        l = 0.f;
+        for (int i = my_row; i < kRows; i += copy_rows)
+          for (int v = 0; v < 2; ++v) {
+            const float2 e = sh.ml[v][i];
+            const float f = e.x == -INFINITY ? (e.y == e.y ? 0.f : e.y) : exp2_fast(e.x - m);
+            l += e.x == -INFINITY ? f : e.y * f;
+            if (i == row) { if (v == 0) factor0 = f; else factor1 = f; }
+          }
       }
-      const bool whole = x.k0 == 0 && x.k1 == w.tiles;
+      const float share = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+      factor0 *= share;
+      factor1 *= share;
+      const int head = w.head * p.group + w.row0 + my_row - node * p.group;
+      const long long part = (2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0)) * kBlockRows;
+      if (live && (two || (s == 0 && row == my_row))) {
+        if (!whole) p.part_ml[part + my_row] = make_float2(m, l);
+        else if (p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      }
+      // Rows go through shared memory, 32 columns of a warp's 32 rows at a time, so that they leave in whole sectors; and, where there are copies, to
+      // be added up.  Without: a group of warps writes its own rows; with one accumulator's rows in both, each group half of the columns.
       __syncwarp();
-      if (warp_live) {
-        const float share = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-        factor0 *= share;
-        factor1 *= share;
-        T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + head * p.a.out_head_stride + column0;
-        const long long part = (2ll * blockIdx.x + (x.k0 == 0 ? 1 : 0)) * kBlockRows + my_row;
-        float *part_o = p.part_o + part * D + column0;
-        bool odd = false;
-        for (int i = 0; i < columns; i += 32) {
-          uint32_t o[32], o1[32];
-          tmem_load32((two ? my_o : tmem + 256 + ((uint32_t)(warp & 3) << 21)) + column0 + i, o);
-          if (!two) tmem_load32(tmem + 384 + ((uint32_t)(warp & 3) << 21) + column0 + i, o1);
+      const int columns = two ? D : D / 2, column0 = two ? 0 : s * (D / 2);
+      auto put = [&](int c, float *to) {    // 32 columns from c on: 8 vectors a row, swizzled
+        uint32_t o[32];
+        tmem_load32((two ? my_o : tmem + 256 + lanes) + c, o);
+        tmem_wait_loads();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(factor0 == 0.f ? 0.f : __uint_as_float(o[j]) * factor0);
+        if (!two) {
+          uint32_t o1[32];
+          tmem_load32(tmem + 384 + lanes + c, o1);
           tmem_wait_loads();
-          float *v = reinterpret_cast<float *>(o);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            v[j] = factor0 == 0.f ? 0.f : v[j] * factor0;
-            if (!two && factor1 != 0.f) v[j] += __uint_as_float(o1[j]) * factor1;
-            odd |= !(fabsf(v[j]) < INFINITY);
-          }
-          if (live && whole) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 8)
-              *reinterpret_cast<uint4 *>(out + i + j) = make_uint4(pack<T>(v[j], v[j + 1]), pack<T>(v[j + 2], v[j + 3]), pack<T>(v[j + 4], v[j + 5]),
-                                                                   pack<T>(v[j + 6], v[j + 7]));
-          } else if (live) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(part_o + i + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-          }
-          __syncwarp();
+          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) + (factor1 == 0.f ? 0.f : __uint_as_float(o1[j]) * factor1));
         }
-        if (live && (two || s == 0)) {
-          if (!whole) p.part_ml[part] = make_float2(m, l);
-          else if (p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-        }
-        // A row with a NaN or an infinity: from a value that the row does not see (0 times it is NaN), or its own.  Once more, key by key.
-        for (uint32_t again = __ballot_sync(~0u, live && odd); again; again &= again - 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          *reinterpret_cast<uint4 *>(to + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+      };
+      // 4 rows at a time, 8 lanes a row: the row r of the block, columns c + 4 (lane & 7) on
+      auto write = [&](int r, int c, float4 v) {
+        const bool there = r < w.rows;
+        const int node_ = token_of(p, w.row0 + min(r, w.rows - 1)), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
+        const int column = c + 4 * (lane & 7);
+        T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
+        float *part_o = p.part_o + (part + r) * D;
+        if (there && whole) *reinterpret_cast<uint2 *>(out + column) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
+        else if (there) *reinterpret_cast<float4 *>(part_o + column) = v;
+        // A NaN or an infinity: from a value that the row does not see (0 times it is NaN), or its own.  These 32 columns once more, key by key.
+        const bool odd = there && !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY);
+        uint32_t again = __ballot_sync(~0u, odd);
+        while (again) {
           const int from = __ffs(again) - 1;
-          const int i_ = __shfl_sync(~0u, node, from), h_ = __shfl_sync(~0u, head, from);
-          const float m_ = __shfl_sync(~0u, m, from), share_ = __shfl_sync(~0u, share, from);
+          again &= ~(0xFFu << (from & ~7));
+          const int r_ = __shfl_sync(~0u, r, from), i_ = token_of(p, w.row0 + r_), h_ = w.head * p.group + w.row0 + r_ - i_ * p.group;
+          const Sight see = sight_of(p, w);
           constexpr int E = D / 32;
           float m2 = -INFINITY, l2 = 0.f, o2[E];
 #pragma unroll
           for (int e = 0; e < E; ++e) o2[e] = 0.f;
-          for (int t = x.k0; t < x.k1; ++t)
-            attend_row<T, D>(p.c, p.a, see, w.b, i_, h_, w.key0(t), min(w.key0(t) + kTile, see.keys), m2, l2, o2);
-          const float to = l2 == 0.f ? 0.f : exp2f(m2 - m_) * share_;
-          const bool mine = two || (lane * E >= column0 && lane * E < column0 + columns);
-          T *out_ = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i_ * p.a.out_token_stride + h_ * p.a.out_head_stride + lane * E;
-          float *part_ = p.part_o + ((2ll * blockIdx.x + (x.k0 == 0 ? 1 : 0)) * kBlockRows + __shfl_sync(~0u, my_row, from)) * D + lane * E;
+          for (int t = w.k0; t < w.k1; ++t)
+            attend_row<T, D>(p.c, p.a, see, w.b, i_, h_, w.key0(t), min(w.key0(t) + kTile, w.keys), m2, l2, o2);
+          float to = whole ? (l2 == 0.f ? 0.f : 1.f / l2) : 1.f;
+          if (!whole) {                     // as the part's other columns: relative to its maximum
+            const float m_ = two ? __shfl_sync(~0u, m, r_ & 31) : row_maximum(sh.ml, r_, copy_rows);
+            to = l2 == 0.f ? 0.f : exp2f(m2 - m_);
+          }
+          T *out_ = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i_ * p.a.out_token_stride + h_ * p.a.out_head_stride;
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            if (!mine) continue;
-            if (whole) out_[e] = from_float<T>(to == 0.f ? 0.f : o2[e] * to);
-            else part_[e] = to == 0.f ? 0.f : o2[e] * to;
+            const int d = lane * E + e;
+            if (d < c || d >= c + 32) continue;
+            const float x = to == 0.f ? 0.f : o2[e] * to;
+            if (whole) out_[d] = from_float<T>(x);
+            else p.part_o[(part + r_) * D + d] = x;
           }
+          __syncwarp();
         }
+      };
+      if (two) {
+        for (int c = 0; c < D && warp_live; c += 32) {
+          put(c, stage);
+          __syncwarp();
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            write((my_row & ~31) + r, c, *reinterpret_cast<const float4 *>(stage + r * 32 + (((lane & 7) ^ (r & 7)) << 2)));
+          }
+          __syncwarp();
+        }
+      } else {
+        for (int c = 0; c < columns && warp_live; c += 32) put(column0 + c, stage + c * 32);
+        if (copy_rows < kRows ? !(ok = all_meet()) : false) break;
+        __syncwarp();
+        const int rows_here = copy_rows / 4;                    // of a warp: all rows of a copy among the group's four
+        const float *group_stage = reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);
+        for (int c = 0; c < columns; c += 32)
+#pragma unroll 1
+          for (int i = 0; i < rows_here; i += 4) {
+            const int r = (warp & 3) * rows_here + i + (lane >> 3);
+            if ((r & ~3) >= w.rows) break;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int at = r; at < kRows; at += copy_rows) {
+              const float4 x = *reinterpret_cast<const float4 *>(group_stage + (at >> 5) * (D * 16) + c * 32 + (at & 31) * 32 + (((lane & 7) ^ (at & 7)) << 2));
+              v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            write(r, column0 + c, v);
+          }
       }
+      block_read(item);
     }
   }
   tmem_fence_before();
@@ -743,22 +968,25 @@ __global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(Params p) {
   constexpr int E = D / 32;
   for (int r = blockIdx.y * kJoinRows + warp; r < min((int)(blockIdx.y + 1) * kJoinRows, w.rows); r += kJoinThreads / 32) {
     auto place = [&](int i) { return (2ll * (cut.z + i) + (i == 0 ? 1 : 0)) * kBlockRows + r; };
-    float m = -INFINITY;
+    float m = -INFINITY, l = 0.f, o[E];
     for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[place(i)].x);
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-    float l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int i = 0; i < n; ++i) {
-      const float2 ml = p.part_ml[place(i)];
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;
-      const float f = exp2f(ml.x - m);
-      const float *from = p.part_o + place(i) * D + lane * E;
-      l += ml.y * f;
+    for (int base = 0; base < n; base += 32) {
+      const float2 ml = base + lane < n ? p.part_ml[place(base + lane)] : make_float2(-INFINITY, 0.f);
+      const float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : exp2f(ml.x - m);               // (of a part that sees nothing; its sums are 0)
+      const float lf = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.y * f;
+#pragma unroll 4
+      for (int i = 0; i < min(32, n - base); ++i) {
+        const float *from = p.part_o + place(base + i) * D + lane * E;
+        const float fi = __shfl_sync(~0u, f, i);
+        l += __shfl_sync(~0u, lf, i);
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += from[e] * f;
+        for (int e = 0; e < E; ++e) o[e] += from[e] * fi;
+      }
     }
-    const int at = w.row0 + r, node = at / p.group, head = cut.y * p.group + at - node * p.group;
+    const int at = w.row0 + r, node = token_of(p, at), head = cut.y * p.group + at - node * p.group;
     T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + head * p.a.out_head_stride + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) out[e] = from_float<T>(l == 0.f ? 0.f : o[e] / l);
@@ -868,7 +1096,8 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.a = *attention;
   p.group = p.a.q_heads / p.c.kv_heads;
   const long long rows = (long long)p.a.max_queries * p.group, blocks = (rows + kBlockRows - 1) / kBlockRows;
-  if (blocks * p.c.batch * p.c.kv_heads > 0x7FFFFFFF) return C2T_ERANGE;
+  if (blocks * p.c.batch * p.c.kv_heads > 0x7FFFFFFF || rows * p.group > 0x7FFFFFFF) return C2T_ERANGE;
+  p.group_inverse = p.group > 1 ? (uint32_t)((0x100000000ull + p.group - 1) / p.group) : 0;
   p.blocks_per_seq = (int)blocks;
   p.box_rows = p.c.page_size < kTile ? p.c.page_size : kTile;
   p.split = blocks * p.c.batch <= kMaxPairs;
