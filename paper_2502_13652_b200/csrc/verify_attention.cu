@@ -192,6 +192,7 @@ struct Deal {
 constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x 128 at most
 constexpr float kRaise = 8.f;
+constexpr int kProducts = 2;                // of 8 powers of two that are not taken by the special-function unit: 2 kProducts / 2
 constexpr int kTries = 1 << 22;             // of a wait, after which the block gives up
 
 template <int D> struct Ring { static constexpr int bytes = kTile * D * 2, n = D == 128 ? 5 : 10; };
@@ -212,6 +213,7 @@ struct alignas(1024) Shared {
   Block block[kBlocks];
   uint32_t tmem;
   int gave_up;
+  uint32_t odd[8];
   long long warp_sum[kThreads / 32], left;
   int pair, head, k0;
 };
@@ -223,6 +225,18 @@ __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t pari
   for (int i = 0; i < kTries; ++i) {
     if (barrier_try(bar, parity)) return true;
     if ((i & 63) == 63 && *(volatile int *)&sh.gave_up) return false;
+  }
+  sh.gave_up = 1;
+  return false;
+}
+
+// The same for a whole warp, whose lanes ask together and go on together.  (Lanes that ask each for itself come back up to 750 cycles apart.)  The loop
+// ends on a vote, which all lanes are known to share: the tensor-memory instructions behind it must be reached by the whole warp at once.
+template <int D>
+__device__ __forceinline__ bool warp_wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
+  for (int i = 0; i < kTries; ++i) {
+    if (__all_sync(~0u, barrier_try(bar, parity))) return true;
+    if ((i & 63) == 63 && __any_sync(~0u, *(volatile int *)&sh.gave_up)) return false;
   }
   sh.gave_up = 1;
   return false;
@@ -298,11 +312,35 @@ __device__ __forceinline__ void add2(float &a, float &b, float x, float y) {
       : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
 
-// the maximum of row r over the accumulators and the row's copies
-__device__ __forceinline__ float row_maximum(const float2 (*ml)[kRows], int r, int copy_rows) {
-  float m = -INFINITY;
-  for (int i = r; i < kRows; i += copy_rows) m = fmaxf(m, fmaxf(ml[0][i].x, ml[1][i].x));
-  return m;
+// 2^x and 2^y by products and sums: x = n + f with n the nearest whole number (added to 1.5 * 2^23 it stands in the low bits), 2^f by a polynomial of
+// degree 5 on [-1/2, 1/2] (equal ripple, 1.6e-7 relative with its rounding, 1 at 0), n added to the exponent.  Below -127, -inf included, it is 0.
+__device__ __forceinline__ void exp2_products(float &x, float &y) {
+  x = fmaxf(x, -127.f);
+  y = fmaxf(y, -127.f);
+  float nx = x, ny = y, px, py;
+  asm("{\n\t.reg .b64 v, n, f, q, c;\n\t"
+      "mov.b64 v, {%4, %5};\n\t"
+      "mov.b64 c, {%6, %6};\n\tadd.rn.f32x2 n, v, c;\n\tmov.b64 {%0, %1}, n;\n\t"
+      "mov.b64 c, {%7, %7};\n\tadd.rn.f32x2 n, n, c;\n\t"
+      "mov.b64 c, {%8, %8};\n\tfma.rn.f32x2 f, n, c, v;\n\t"
+      "mov.b64 q, {%9, %9};\n\tmov.b64 c, {%10, %10};\n\tfma.rn.f32x2 q, q, f, c;\n\t"
+      "mov.b64 c, {%11, %11};\n\tfma.rn.f32x2 q, q, f, c;\n\t"
+      "mov.b64 c, {%12, %12};\n\tfma.rn.f32x2 q, q, f, c;\n\t"
+      "mov.b64 c, {%13, %13};\n\tfma.rn.f32x2 q, q, f, c;\n\t"
+      "mov.b64 c, {%14, %14};\n\tfma.rn.f32x2 q, q, f, c;\n\t"
+      "mov.b64 {%2, %3}, q;\n\t}"
+      : "=f"(nx), "=f"(ny), "=f"(px), "=f"(py)
+      : "f"(x), "f"(y), "f"(12582912.f), "f"(-12582912.f), "f"(-1.f), "f"(0.0013274633f), "f"(0.009671962f), "f"(0.055506784f), "f"(0.24022235f),
+        "f"(0.69314706f), "f"(1.f));
+  x = __int_as_float(__float_as_int(px) + (__float_as_int(nx) << 23));
+  y = __int_as_float(__float_as_int(py) + (__float_as_int(ny) << 23));
+}
+
+// the larger one; NaN if any is
+__device__ __forceinline__ float larger(float a, float b) {
+  float x;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
+  return x;
 }
 
 // logits whose bit (from `first` on) is not set become -inf
@@ -348,6 +386,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int f
       const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
       const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
       if (raise) { l *= factor; m = highest; }
+      __syncwarp();
       if (__any_sync(~0u, raise) && has_sums) {
 #pragma unroll 1
         for (int i = 0; i < D; i += 16) {
@@ -360,6 +399,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int f
       }
     }
     const float shift = m == -INFINITY ? 0.f : -m * unit;
+    __syncwarp();
     float top[2] = {-INFINITY, -INFINITY};
     sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
     tmem_load16(from, r[0]);
@@ -372,22 +412,27 @@ __device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int f
 #pragma unroll
       for (int j = 0; j < 16; j += 4) {
         float a = __uint_as_float(y[j]), b = __uint_as_float(y[j + 1]), c = __uint_as_float(y[j + 2]), d = __uint_as_float(y[j + 3]);
-        top[0] = fmaxf(fmaxf(top[0], a), b);
-        top[1] = fmaxf(fmaxf(top[1], c), d);
+        top[0] = larger(larger(top[0], a), b);
+        top[1] = larger(larger(top[1], c), d);
         scale_add2(a, b, unit, shift);
         scale_add2(c, d, unit, shift);
-        a = exp2_fast(a); b = exp2_fast(b); c = exp2_fast(c); d = exp2_fast(d);
+        a = exp2_fast(a); b = exp2_fast(b);
+        if (((4 * i + j / 4) & 3) < kProducts) exp2_products(c, d);
+        else { c = exp2_fast(c); d = exp2_fast(d); }
         add2(sum[0], sum[1], a, b);
         add2(sum[2], sum[3], c, d);
         packed[8 * i + j / 2] = pack<T>(a, b);
         packed[8 * i + j / 2 + 1] = pack<T>(c, d);
       }
     }
+    const float highest = larger(top[0], top[1]);
+    if (!(highest < INFINITY)) l = NAN;     // (a logit that is none makes the row NaN, whichever way its power was taken)
     if (known) break;
-    known = again = __any_sync(~0u, (fmaxf(top[0], top[1]) - m) * unit > kRaise);
+    known = again = __any_sync(~0u, (highest - m) * unit > kRaise);
     if (!again) break;
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  __syncwarp();
 #pragma unroll
   for (int i = 0; i < kChunks; i += 2) tmem_store16(my_s + first / 2 + 8 * i, packed + 8 * i);
   if (kChunks < 8) {                        // the keys of the other copies
@@ -535,7 +580,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   const uint32_t tmem = sh.tmem;
 
   // the i-th block of rows of the share; rows = 0 behind the last
-  auto described = [&](int i) { return wait(sh, sh.described + i % kBlocks, i / kBlocks & 1); };
+  auto described = [&](int i) {
+    if (!warp_wait(sh, sh.described + i % kBlocks, i / kBlocks & 1)) return false;
+#ifdef C2T_DEBUG_BOUNDS
+    const Block &w = sh.block[i % kBlocks];
+    if (w.rows != 0 && (w.b < 0 || w.b >= p.c.batch || w.head < 0 || w.head >= p.c.kv_heads || w.row0 < 0 || w.rows < 0 || w.rows > kBlockRows || w.k0 < 0 ||
+                        w.k1 <= w.k0 || w.k1 > w.tiles || w.n > p.a.max_queries || w.row0 + w.rows > w.n * p.group)) {
+      if (p.c.status_dev) atomicOr(p.c.status_dev, C2T_ST_INTERNAL);
+      sh.gave_up = 1;
+      return false;
+    }
+#endif
+    return true;
+  };
   auto block_read = [&](int i) {
     __syncwarp();
     if (lane == 0) barrier_arrive(sh.read + i % kBlocks);
@@ -589,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     int filled = 0;
     bool ok = true;
     for (int item = 0;; ++item) {
-      if (!(ok = __all_sync(~0u, described(item)))) break;
+      if (!(ok = described(item))) break;
       const Block w = sh.block[item % kBlocks];
       block_read(item);
       if (w.rows == 0) break;
@@ -608,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       int key, next_key, page = page_of(0, values, key);
       for (int i = 0; i < 2 * n; ++i) {
         const int next = page_of(i + 1, next_values, next_key);
-        ok = __all_sync(~0u, wait(sh, sh.empty + to.at, to.parity ^ 1));
+        ok = warp_wait(sh, sh.empty + to.at, to.parity ^ 1);
         if (!ok) break;
         if (lane == 0) barrier_expect(sh.full + to.at, Ring<D>::bytes);
         if (page < 0 || page > p.c.n_pages || (page == p.c.n_pages && key < w.keys && lane < boxes)) {
@@ -643,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     uint32_t weights_parity[2] = {0, 0};
     bool ok = true;
     int item = 0;
-    auto arrived = [&](uint64_t *bar, uint32_t parity) { return __all_sync(~0u, wait(sh, bar, parity)) != 0; };
+    auto arrived = [&](uint64_t *bar, uint32_t parity) { return warp_wait(sh, bar, parity); };
     auto logits = [&](int s, int half, int buffer) {
       const uint64_t a = q_tile + half * (kRows * D * 2 / 16), b = k_tile + (uint32_t)buffer * (Ring<D>::bytes / 16);
       if (leader) {
@@ -752,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     int item = 0, turn = 0;                 // buffers of the ring so far
     auto all_meet = [&] {
       barrier_arrive(&sh.meet);
-      const bool met = wait(sh, &sh.meet, meet_parity);
+      const bool met = warp_wait(sh, &sh.meet, meet_parity);
       meet_parity ^= 1;
       return met;
     };
@@ -793,11 +850,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
               on[0] = sight_bits(see, node, own, key + first_column + 32 * (i - 1));
             }
           }
-          if (!(ok = wait(sh, sh.logits + s, logits_parity))) break;
+          if (!(ok = warp_wait(sh, sh.logits + s, logits_parity))) break;
           logits_parity ^= 1;
           tmem_fence_after();
           if (key + kTile > see.keys) {     // rows of the values that nobody wrote: their weights are 0, they must be numbers
-            if (!(ok = wait(sh, sh.full + vals_at.at, vals_at.parity))) break;
+            if (!(ok = warp_wait(sh, sh.full + vals_at.at, vals_at.parity))) break;
             if (key + row >= see.keys && !(two && s == 1)) {    // (the first group's are in time for both)
 #pragma unroll
               for (int i = 0; i < D / 8; ++i)
@@ -818,7 +875,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           barrier_arrive(sh.weights + s);
         }
       }
-      if (!ok || !(ok = wait(sh, &sh.done, item & 1))) {
+      if (!ok || !(ok = warp_wait(sh, &sh.done, item & 1))) {
         if (tid == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
         break;
       }
@@ -831,119 +888,137 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       const bool whole = w.k0 == 0 && w.k1 == w.tiles;
       m = m == -INFINITY ? m : m * unit;
       float factor0 = 1.f, factor1 = 0.f;
-      if (!two) {                           // over the two accumulators and the copies of the row
+      if (!two) {                           // over the two accumulators and, for a finished row, its copies
         sh.ml[s][row] = make_float2(m, l);
         if (!(ok = all_meet())) break;
+        const int lane_row = whole ? my_row : row, step = whole ? copy_rows : kRows;
         m = -INFINITY;
-        for (int i = my_row; i < kRows; i += copy_rows) m = fmaxf(m, fmaxf(sh.ml[0][i].x, sh.ml[1][i].x));
+        for (int i = lane_row; i < kRows; i += step) m = fmaxf(m, fmaxf(sh.ml[0][i].x, sh.ml[1][i].x));
         l = 0.f;
-        for (int i = my_row; i < kRows; i += copy_rows)
+        for (int i = lane_row; i < kRows; i += step)
           for (int v = 0; v < 2; ++v) {
             const float2 e = sh.ml[v][i];
-            const float f = e.x == -INFINITY ? (e.y == e.y ? 0.f : e.y) : exp2_fast(e.x - m);
-            l += e.x == -INFINITY ? f : e.y * f;
+            const float f = e.x == -INFINITY ? 0.f : exp2_fast(e.x - m);
+            l += e.x == -INFINITY ? e.y : e.y * f;              // (0, or NaN)
             if (i == row) { if (v == 0) factor0 = f; else factor1 = f; }
           }
       }
       const float share = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
       factor0 *= share;
       factor1 *= share;
+      if (l != l) factor0 = l;
       const int head = w.head * p.group + w.row0 + my_row - node * p.group;
-      const long long part = (2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0)) * kBlockRows;
-      if (live && (two || (s == 0 && row == my_row))) {
-        if (!whole) p.part_ml[part + my_row] = make_float2(m, l);
-        else if (p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-      }
-      // Rows go through shared memory, 32 columns of a warp's 32 rows at a time, so that they leave in whole sectors; and, where there are copies, to
-      // be added up.  Without: a group of warps writes its own rows; with one accumulator's rows in both, each group half of the columns.
+      const long long part = 2ll * blockIdx.x + (w.k0 == 0 ? 1 : 0);
+      const int columns = two ? D : D / 2, column0 = two ? 0 : s * (D / 2);     // of both accumulators each group takes half
       __syncwarp();
-      const int columns = two ? D : D / 2, column0 = two ? 0 : s * (D / 2);
-      auto put = [&](int c, float *to) {    // 32 columns from c on: 8 vectors a row, swizzled
-        uint32_t o[32];
+      auto sums = [&](int c, float *v) {    // this lane's 32 columns from c on; the whole warp
+        uint32_t *o = reinterpret_cast<uint32_t *>(v);
+        __syncwarp();
         tmem_load32((two ? my_o : tmem + 256 + lanes) + c, o);
+        uint32_t o1[32];
+        if (!two) tmem_load32(tmem + 384 + lanes + c, o1);
         tmem_wait_loads();
+        bool fine = true;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(factor0 == 0.f ? 0.f : __uint_as_float(o[j]) * factor0);
-        if (!two) {
-          uint32_t o1[32];
-          tmem_load32(tmem + 384 + lanes + c, o1);
-          tmem_wait_loads();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) + (factor1 == 0.f ? 0.f : __uint_as_float(o1[j]) * factor1));
+        for (int j = 0; j < 32; ++j) {
+          v[j] = factor0 == 0.f ? 0.f : v[j] * factor0;
+          if (!two && factor1 != 0.f) v[j] = fmaf(__uint_as_float(o1[j]), factor1, v[j]);
+          fine &= fabsf(v[j]) < INFINITY;
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          *reinterpret_cast<uint4 *>(to + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        return fine;
       };
-      // 4 rows at a time, 8 lanes a row: the row r of the block, columns c + 4 (lane & 7) on
-      auto write = [&](int r, int c, float4 v) {
-        const bool there = r < w.rows;
-        const int node_ = token_of(p, w.row0 + min(r, w.rows - 1)), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
-        const int column = c + 4 * (lane & 7);
-        T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
-        float *part_o = p.part_o + (part + r) * D;
-        if (there && whole) *reinterpret_cast<uint2 *>(out + column) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
-        else if (there) *reinterpret_cast<float4 *>(part_o + column) = v;
-        // A NaN or an infinity: from a value that the row does not see (0 times it is NaN), or its own.  These 32 columns once more, key by key.
-        const bool odd = there && !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY);
-        uint32_t again = __ballot_sync(~0u, odd);
-        while (again) {
+      // A NaN or an infinity: from a value that the row does not see (0 times it is NaN), or its own.  The row once more, key by key: those of the
+      // tiles that lie in [first, first + size) of each; in units of the share, or relative to the part's maximum.
+      auto once_more = [&](int r, int first, int size, bool finish, float part_m, float *to_part) {
+        const int i_ = token_of(p, w.row0 + r), h_ = w.head * p.group + w.row0 + r - i_ * p.group;
+        const Sight see = sight_of(p, w);
+        constexpr int E = D / 32;
+        float m2 = -INFINITY, l2 = 0.f, o2[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o2[e] = 0.f;
+        for (int t = w.k0; t < w.k1; ++t)
+          attend_row<T, D>(p.c, p.a, see, w.b, i_, h_, w.key0(t) + first, min(w.key0(t) + first + size, w.keys), m2, l2, o2);
+        const float f = l2 == 0.f ? 0.f : finish ? 1.f / l2 : exp2f(m2 - part_m);
+        T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i_ * p.a.out_token_stride + h_ * p.a.out_head_stride;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int d = lane * E + e;
+          const float x = f == 0.f ? 0.f : o2[e] * f;
+          if (d < column0 || d >= column0 + columns) continue;
+          if (finish) out[d] = from_float<T>(x);
+          else to_part[(d >> 2) * (kBlockRows * 4) + (d & 3)] = x;
+        }
+        __syncwarp();
+      };
+
+      if (!whole) {
+        // a part: 16 bytes a lane, the rows side by side
+        const int place = two ? my_row : row;
+        float *to = p.part_o + (part * (D / 4) * kBlockRows + place) * 4;
+        bool fine = true;
+        for (int c = 0; c < columns && warp_live; c += 32) {
+          float v[32];
+          fine &= sums(column0 + c, v);
+#pragma unroll
+          for (int j = 0; j < 32; j += 4)
+            if (live) *reinterpret_cast<float4 *>(to + (column0 + c + j) * kBlockRows) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          __syncwarp();
+        }
+        if (live && (two || s == 0)) p.part_ml[part * kBlockRows + place] = make_float2(m, l);
+        for (uint32_t again = __ballot_sync(~0u, live && !fine); again; again &= again - 1) {
           const int from = __ffs(again) - 1;
-          again &= ~(0xFFu << (from & ~7));
-          const int r_ = __shfl_sync(~0u, r, from), i_ = token_of(p, w.row0 + r_), h_ = w.head * p.group + w.row0 + r_ - i_ * p.group;
-          const Sight see = sight_of(p, w);
-          constexpr int E = D / 32;
-          float m2 = -INFINITY, l2 = 0.f, o2[E];
-#pragma unroll
-          for (int e = 0; e < E; ++e) o2[e] = 0.f;
-          for (int t = w.k0; t < w.k1; ++t)
-            attend_row<T, D>(p.c, p.a, see, w.b, i_, h_, w.key0(t), min(w.key0(t) + kTile, w.keys), m2, l2, o2);
-          float to = whole ? (l2 == 0.f ? 0.f : 1.f / l2) : 1.f;
-          if (!whole) {                     // as the part's other columns: relative to its maximum
-            const float m_ = two ? __shfl_sync(~0u, m, r_ & 31) : row_maximum(sh.ml, r_, copy_rows);
-            to = l2 == 0.f ? 0.f : exp2f(m2 - m_);
-          }
-          T *out_ = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i_ * p.a.out_token_stride + h_ * p.a.out_head_stride;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int d = lane * E + e;
-            if (d < c || d >= c + 32) continue;
-            const float x = to == 0.f ? 0.f : o2[e] * to;
-            if (whole) out_[d] = from_float<T>(x);
-            else p.part_o[(part + r_) * D + d] = x;
-          }
-          __syncwarp();
-        }
-      };
-      if (two) {
-        for (int c = 0; c < D && warp_live; c += 32) {
-          put(c, stage);
-          __syncwarp();
-#pragma unroll 1
-          for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + (lane >> 3);
-            write((my_row & ~31) + r, c, *reinterpret_cast<const float4 *>(stage + r * 32 + (((lane & 7) ^ (r & 7)) << 2)));
-          }
-          __syncwarp();
+          once_more(__shfl_sync(~0u, my_row, from), two ? 0 : first_column, two ? kTile : copy_rows, false, __shfl_sync(~0u, m, from),
+                    p.part_o + (part * (D / 4) * kBlockRows + __shfl_sync(~0u, place, from)) * 4);
         }
       } else {
-        for (int c = 0; c < columns && warp_live; c += 32) put(column0 + c, stage + c * 32);
-        if (copy_rows < kRows ? !(ok = all_meet()) : false) break;
-        __syncwarp();
-        const int rows_here = copy_rows / 4;                    // of a warp: all rows of a copy among the group's four
-        const float *group_stage = reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);
-        for (int c = 0; c < columns; c += 32)
-#pragma unroll 1
+        // Finished rows go through shared memory, so that they leave in whole sectors and their copies are added up: a warp's 32 rows, 32 columns
+        // at a time, 8 vectors a row, swizzled.  4 rows leave at a time, 8 lanes a row.
+        if (p.a.lse_dev && live && (two || (s == 0 && row == my_row)))
+          p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        bool fine = true;
+        const int rows_here = two ? 32 : copy_rows / 4, r0 = two ? my_row & ~31 : (warp & 3) * rows_here;
+        const float *from = two ? stage : reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);
+        auto put = [&](int c, float *to) {
+          float v[32];
+          fine &= sums(c, v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4 *>(to + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        };
+        auto write = [&](int c, const float *chunk) {           // 32 columns from c on
+#pragma unroll 4
           for (int i = 0; i < rows_here; i += 4) {
-            const int r = (warp & 3) * rows_here + i + (lane >> 3);
-            if ((r & ~3) >= w.rows) break;
+            const int r = r0 + i + (lane >> 3), at = two ? r & 31 : r;
+            if (r >= w.rows) break;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int at = r; at < kRows; at += copy_rows) {
-              const float4 x = *reinterpret_cast<const float4 *>(group_stage + (at >> 5) * (D * 16) + c * 32 + (at & 31) * 32 + (((lane & 7) ^ (at & 7)) << 2));
+            for (int a = at; a < (two ? 32 : kRows); a += two ? 32 : copy_rows) {
+              const float4 x = *reinterpret_cast<const float4 *>(chunk + (a >> 5) * (D * 16) + (a & 31) * 32 + (((lane & 7) ^ (a & 7)) << 2));
               v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
             }
-            write(r, column0 + c, v);
+            const int node_ = token_of(p, w.row0 + r), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
+            T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
+            *reinterpret_cast<uint2 *>(out + c + 4 * (lane & 7)) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
           }
+          __syncwarp();
+        };
+        if (two) {
+          for (int c = 0; c < D && warp_live; c += 32) {
+            put(c, stage);
+            __syncwarp();
+            write(c, from);
+          }
+        } else {
+          for (int c = 0; c < columns && warp_live; c += 32) put(column0 + c, stage + c * 32);
+          const uint32_t odd = __ballot_sync(~0u, live && !fine);
+          if (lane == 0) sh.odd[warp] = odd;
+          if (copy_rows < kRows && !(ok = all_meet())) break;
+          __syncwarp();
+          for (int c = 0; c < columns; c += 32) write(column0 + c, from + c * 32);
+          fine = true;
+          for (int a = r0 + lane; a < kRows && lane < rows_here; a += copy_rows) fine &= !(sh.odd[s * 4 + (a >> 5)] >> (a & 31) & 1);
+        }
+        for (uint32_t again = __ballot_sync(~0u, !fine && r0 + lane < w.rows); again; again &= again - 1)
+          once_more(r0 + __ffs(again) - 1, 0, kTile, true, 0.f, nullptr);
       }
       block_read(item);
     }
@@ -955,44 +1030,69 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 
 // ---------------------------------------------------------------- parts of rows that several thread blocks read the keys of
 
-constexpr int kJoinThreads = 128, kJoinRows = 8;                // rows of a thread block, two a warp
+constexpr int kJoinThreads = 128;           // a quarter of the columns a warp
 
 // Grid (G, parts of a block's rows).  The parts of a cut block of rows lie with thread blocks c0 .. c1: the first's second place, then the others' first.
-template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(Params p) {
+// Of a part, 16 bytes of all rows lie side by side.  Rows that lay in the accumulators in copies have a part for each.
+// kJoinRows lanes have a row each, and the 32 / kJoinRows lanes of a row every so many-th of its parts: with few rows the parts, one after the other, are
+// what the launch would wait for.
+template <typename T, int D, int kJoinRows>
+__global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(const __grid_constant__ Params p) {
   chain_enter();
   const int4 cut = p.cut[blockIdx.x];
   if (cut.x < 0) return;
   const Block w = block_of(p, cut.x);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = cut.w - cut.z + 1;
-  constexpr int E = D / 32;
-  for (int r = blockIdx.y * kJoinRows + warp; r < min((int)(blockIdx.y + 1) * kJoinRows, w.rows); r += kJoinThreads / 32) {
-    auto place = [&](int i) { return (2ll * (cut.z + i) + (i == 0 ? 1 : 0)) * kBlockRows + r; };
-    float m = -INFINITY, l = 0.f, o[E];
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[place(i)].x);
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int base = 0; base < n; base += 32) {
-      const float2 ml = base + lane < n ? p.part_ml[place(base + lane)] : make_float2(-INFINITY, 0.f);
-      const float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : exp2f(ml.x - m);               // (of a part that sees nothing; its sums are 0)
-      const float lf = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.y * f;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * kJoinRows + lane % kJoinRows;
+  const bool there = r < w.rows;
+  const int shift = w.rows > kRows ? 0 : w.rows <= 32 ? 2 : w.rows <= 64 ? 1 : 0, copy_rows = kRows >> shift;
+  const int n = there ? (cut.w - cut.z + 1) << shift : 0;
+  constexpr int kColumns = D / 4;           // of a warp
+  // the i-th part: its thread block's place, and the row's among its rows
+  auto place = [&](int i) {
+    const int c = cut.z + (i >> shift);
+    return (2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows * (D / 4) + (r + (i & ((1 << shift) - 1)) * copy_rows);
+  };
+  auto ml_of = [&](int i) {
+    const int c = cut.z + (i >> shift);
+    return p.part_ml[(2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows + r + (i & ((1 << shift) - 1)) * copy_rows];
+  };
+  float m = -INFINITY, l = 0.f;
 #pragma unroll 4
-      for (int i = 0; i < min(32, n - base); ++i) {
-        const float *from = p.part_o + place(base + i) * D + lane * E;
-        const float fi = __shfl_sync(~0u, f, i);
-        l += __shfl_sync(~0u, lf, i);
+  for (int i = lane / kJoinRows; i < n; i += 32 / kJoinRows) m = fmaxf(m, ml_of(i).x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += from[e] * fi;
-      }
+  for (int d = kJoinRows; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+  float o[kColumns];
+#pragma unroll
+  for (int j = 0; j < kColumns; ++j) o[j] = 0.f;
+#pragma unroll 2
+  for (int i = lane / kJoinRows; i < n; i += 32 / kJoinRows) {
+    const float2 ml = ml_of(i);
+    const float4 *from = reinterpret_cast<const float4 *>(p.part_o) + place(i) + warp * (kColumns / 4) * kBlockRows;
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+    l += ml.x == -INFINITY ? ml.y : ml.y * f;                   // (a part that sees nothing: 0, or NaN)
+#pragma unroll
+    for (int j = 0; j < kColumns; j += 4) {
+      const float4 x = from[(j / 4) * kBlockRows];
+      o[j] = fmaf(x.x, f, o[j]); o[j + 1] = fmaf(x.y, f, o[j + 1]); o[j + 2] = fmaf(x.z, f, o[j + 2]); o[j + 3] = fmaf(x.w, f, o[j + 3]);
     }
-    const int at = w.row0 + r, node = token_of(p, at), head = cut.y * p.group + at - node * p.group;
-    T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + head * p.a.out_head_stride + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = from_float<T>(l == 0.f ? 0.f : o[e] / l);
-    if (p.a.lse_dev && lane == 0)
-      p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
+#pragma unroll
+  for (int d = kJoinRows; d < 32; d <<= 1) {
+    l += __shfl_xor_sync(~0u, l, d);
+#pragma unroll
+    for (int j = 0; j < kColumns; ++j) o[j] += __shfl_xor_sync(~0u, o[j], d);
+  }
+  if (!there) return;
+  const int at = w.row0 + r, node = token_of(p, at), head = cut.y * p.group + at - node * p.group;
+  const float share = l == 0.f ? 0.f : 1.f / l;
+  T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + head * p.a.out_head_stride + warp * kColumns;
+  if (lane < kJoinRows)
+#pragma unroll
+    for (int j = 0; j < kColumns; j += 8)
+      *reinterpret_cast<uint4 *>(out + j) = make_uint4(pack<T>(o[j] * share, o[j + 1] * share), pack<T>(o[j + 2] * share, o[j + 3] * share),
+                                                       pack<T>(o[j + 4] * share, o[j + 5] * share), pack<T>(o[j + 6] * share, o[j + 7] * share));
+  if (p.a.lse_dev && warp == 0 && lane < kJoinRows)
+    p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 int check_attention(const c2t_cache *c, const c2t_attention *a) {
@@ -1066,8 +1166,9 @@ cudaError_t launch_attention(const Params &p, const Maps &maps, int sms, cudaStr
   if (e == cudaSuccess) e = launch_chained(attend_tiles_kernel<T, D>, dim3(sms), dim3(kThreads), smem, s, maps, p);
   if (e == cudaSuccess && p.split) {
     const long long rows = (long long)p.a.max_queries * p.group;
-    const unsigned parts = (unsigned)((rows < kBlockRows ? rows : kBlockRows) + kJoinRows - 1) / kJoinRows;
-    e = launch_chained(join_parts_kernel<T, D>, dim3(sms, parts), dim3(kJoinThreads), 0, s, p);
+    const int most = (int)(rows < kBlockRows ? rows : kBlockRows);
+    if (most <= 32) e = launch_chained(join_parts_kernel<T, D, 8>, dim3(sms, (most + 7) / 8), dim3(kJoinThreads), 0, s, p);
+    else e = launch_chained(join_parts_kernel<T, D, 32>, dim3(sms, (most + 31) / 32), dim3(kJoinThreads), 0, s, p);
   }
   return e;
 }
