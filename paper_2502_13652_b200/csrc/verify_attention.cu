@@ -161,18 +161,16 @@ __device__ __forceinline__ Sight sight_of(const Params &p, const Block &w) {
 
 // An even deal of `total` tiles to `used` thread blocks: the first `more` of them get one more than the others.
 struct Deal {
-  long long total;
-  int used, more;
-  long long each;
-  __device__ __forceinline__ Deal(long long total_, int grid) : total(total_) {
-    used = (int)min(max(total, 1ll), (long long)grid);          // (none without a tile)
-    each = total < 0x7FFFFFFF ? (uint32_t)total / (uint32_t)used : total / used;
-    more = (int)(total - each * used);
+  int total, used, each, more;
+  __device__ __forceinline__ Deal(int total_, int grid) : total(total_) {
+    used = min(max(total, 1), grid);        // (none without a tile)
+    each = total / used;
+    more = total - each * used;
   }
-  __device__ __forceinline__ long long begin(int c) const { return c >= used ? total : c * each + min(c, more); }
-  __device__ __forceinline__ int owner(long long x) const {     // of tile x
-    const long long wide = more * (each + 1), y = x < wide ? x : x - wide, by = x < wide ? each + 1 : each;
-    return (x < wide ? 0 : more) + (int)(y < 0x7FFFFFFF ? (uint32_t)y / (uint32_t)by : y / by);
+  __device__ __forceinline__ int begin(int c) const { return c >= used ? total : c * each + min(c, more); }
+  __device__ __forceinline__ int owner(int x) const {           // of tile x
+    const int wide = more * (each + 1);
+    return x < wide ? x / (each + 1) : more + (x - wide) / each;
   }
 };
 
@@ -205,7 +203,7 @@ struct alignas(1024) Shared {
   unsigned char q[2][kRows * D * 2];        // 64 elements of all rows after the other 64; at a block's end its sums over the values
   union {
     unsigned char ring[Ring<D>::n][Ring<D>::bytes];
-    long long before[C2T_MAX_BATCH + 1];    // while the work is dealt out: tiles of the pairs before
+    int before[C2T_MAX_BATCH + 1];          // while the work is dealt out: tiles of the pairs before
   };
   float2 ml[2][kRows];
   uint64_t full[Ring<D>::n], empty[Ring<D>::n];
@@ -214,8 +212,7 @@ struct alignas(1024) Shared {
   uint32_t tmem;
   int gave_up;
   uint32_t odd[8];
-  long long warp_sum[kThreads / 32], left;
-  int pair, head, k0;
+  int warp_sum[kThreads / 32], left, pair, head, k0;
 };
 
 constexpr int kMaxPairs = C2T_MAX_BATCH;    // for an even deal
@@ -254,6 +251,14 @@ struct Cursor {
 };
 __device__ __forceinline__ int step_of_keys(int t, int ahead) { return t + 1 < ahead ? 1 : 2; }              // from K_t to K_{t+1}
 __device__ __forceinline__ int step_of_values(int t, int n, int ahead) { return t + ahead < n ? 2 : 1; }     // from V_t to V_{t+1}
+
+// Of the box that holds a sequence's last key only the rows up to that key are copied, to the box's end; the rows before them read as zeros, or as earlier
+// keys.  (What lies behind the last key in its page may be anything, and 0 times anything need not be 0.)  With `there` keys of the sequence from
+// a tile's first on: the column at which that box begins, kTile if the tile has none; and by how many columns its keys are further right.
+__device__ __forceinline__ int last_box(int there, int box_rows) { return there >= kTile || there <= 0 ? kTile : (there - 1) & -box_rows; }
+__device__ __forceinline__ int shift_of_last_box(int there, int box_rows) {
+  return there >= kTile || there <= 0 ? 0 : last_box(there, box_rows) + box_rows - there;
+}
 
 // bits 0..31: columns c < n
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
@@ -343,11 +348,11 @@ __device__ __forceinline__ float larger(float a, float b) {
   return x;
 }
 
-// logits whose bit (from `first` on) is not set become -inf
-__device__ __forceinline__ void mask16(bool masked, uint32_t on, int first, uint32_t *y) {
+// logits whose bit is not set become -inf
+__device__ __forceinline__ void mask32(bool masked, uint32_t on, uint32_t *y) {
   if (!masked) return;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) y[j] = on >> (first + j) & 1 ? y[j] : 0xFF800000u;
+  for (int j = 0; j < 32; ++j) y[j] = on >> j & 1 ? y[j] : 0xFF800000u;
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
@@ -360,89 +365,73 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
   return *reinterpret_cast<const uint32_t *>(&x);
 }
 
-// A row's softmax over 16 * kChunks of a tile's logits, from column `first` on.  16 logits at a time.  Once a row has a maximum the weights are
-// computed with it at once, and their own maximum is taken on the way: it hardly ever asks for another one.
-template <typename T, int D, int kChunks>
-__device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int first, bool masked, const uint32_t *on, float unit, bool has_sums, float &m,
-                                             float &l) {
-  uint32_t r[2][16], packed[8 * kChunks];
-  const uint32_t from = my_s + first;
-  bool known = __any_sync(~0u, m == -INFINITY), again = known;
-  float sum[4];
-  for (;;) {
-    if (again) {
-      float top[2] = {-INFINITY, -INFINITY};
-      tmem_load16(from, r[0]);
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        tmem_wait_loads();
-        if (i + 1 < kChunks) tmem_load16(from + 16 * (i + 1), r[(i + 1) & 1]);
-        mask16(masked, on[i >> 1], (i & 1) * 16, r[i & 1]);
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) top[(j >> 1) & 1] = fmaxf(fmaxf(top[(j >> 1) & 1], __uint_as_float(r[i & 1][j])), __uint_as_float(r[i & 1][j + 1]));
-      }
-      const float highest = fmaxf(top[0], top[1]);
-      // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
-      const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
-      const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
-      if (raise) { l *= factor; m = highest; }
-      __syncwarp();
-      if (__any_sync(~0u, raise) && has_sums) {
+// A row's softmax over `words` * 32 of a tile's logits, from column `first` on: their maximum, then the weights, 32 at a time.  Reading tensor memory twice
+// costs less than holding 128 logits, and a loop less than the same unrolled: the whole kernel has to stay in the instruction cache (at 200 KB of
+// instructions a tile with masks, which comes once per block of rows, took 5000 to 25000 cycles to be fetched).
+template <typename T, int D>
+__device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int first, int words, bool masked, uint32_t on0, uint32_t on1, uint32_t on2,
+                                             uint32_t on3, float unit, bool has_sums, float &m, float &l) {
+  uint32_t y[32];
+  float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-        for (int i = 0; i < D; i += 16) {
-          tmem_load16(my_o + i, r[0]);
-          tmem_wait_loads();
+  for (int i = 0; i < words; ++i) {
+    tmem_load32(my_s + first + 32 * i, y);
+    tmem_wait_loads();
+    mask32(masked, i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3, y);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) r[0][j] = __float_as_uint(__uint_as_float(r[0][j]) * factor);
-          tmem_store16(my_o + i, r[0]);
-        }
-      }
+    for (int j = 0; j < 32; j += 4) {
+      top[0] = larger(larger(top[0], __uint_as_float(y[j])), __uint_as_float(y[j + 1]));
+      top[1] = larger(larger(top[1], __uint_as_float(y[j + 2])), __uint_as_float(y[j + 3]));
     }
-    const float shift = m == -INFINITY ? 0.f : -m * unit;
-    __syncwarp();
-    float top[2] = {-INFINITY, -INFINITY};
-    sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
-    tmem_load16(from, r[0]);
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
+  }
+  const float highest = larger(top[0], top[1]);
+  if (!(highest < INFINITY)) l = NAN;       // (a logit that is none makes the row NaN, whichever way its power is taken)
+  // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
+  const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
+  const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
+  if (raise) { l *= factor; m = highest; }
+  if (__any_sync(~0u, raise) && has_sums) {
+#pragma unroll 1
+    for (int i = 0; i < D; i += 32) {
+      tmem_load32(my_o + i, y);
       tmem_wait_loads();
-      if (i + 1 < kChunks) tmem_load16(from + 16 * (i + 1), r[(i + 1) & 1]);
-      uint32_t *y = r[i & 1];
-      mask16(masked, on[i >> 1], (i & 1) * 16, y);
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
+      for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * factor);
+      tmem_store32(my_o + i, y);
+    }
+  }
+  const float shift = m == -INFINITY ? 0.f : -m * unit;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int column = first + 32 * i;      // (words = 4: in order, so that no logits are overwritten that are still to be read)
+    uint32_t packed[16];
+    if (i < words) {
+      __syncwarp();
+      tmem_load32(my_s + column, y);
+      tmem_wait_loads();
+      mask32(masked, i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3, y);
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) {
         float a = __uint_as_float(y[j]), b = __uint_as_float(y[j + 1]), c = __uint_as_float(y[j + 2]), d = __uint_as_float(y[j + 3]);
-        top[0] = larger(larger(top[0], a), b);
-        top[1] = larger(larger(top[1], c), d);
         scale_add2(a, b, unit, shift);
         scale_add2(c, d, unit, shift);
         a = exp2_fast(a); b = exp2_fast(b);
-        if (((4 * i + j / 4) & 3) < kProducts) exp2_products(c, d);
+        if (((j / 4) & 3) < kProducts) exp2_products(c, d);
         else { c = exp2_fast(c); d = exp2_fast(d); }
         add2(sum[0], sum[1], a, b);
         add2(sum[2], sum[3], c, d);
-        packed[8 * i + j / 2] = pack<T>(a, b);
-        packed[8 * i + j / 2 + 1] = pack<T>(c, d);
+        packed[j / 2] = pack<T>(a, b);
+        packed[j / 2 + 1] = pack<T>(c, d);
       }
+    } else {                                // the keys of the other copies
+#pragma unroll
+      for (int j = 0; j < 16; ++j) packed[j] = 0;
     }
-    const float highest = larger(top[0], top[1]);
-    if (!(highest < INFINITY)) l = NAN;     // (a logit that is none makes the row NaN, whichever way its power was taken)
-    if (known) break;
-    known = again = __any_sync(~0u, (highest - m) * unit > kRaise);
-    if (!again) break;
+    __syncwarp();
+    tmem_store16(my_s + (column & (kTile - 1)) / 2, packed);
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < kChunks; i += 2) tmem_store16(my_s + first / 2 + 8 * i, packed + 8 * i);
-  if (kChunks < 8) {                        // the keys of the other copies
-    uint32_t zero[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) zero[i] = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2)
-      if (i * 16 < first || i * 16 >= first + kChunks * 16) tmem_store16(my_s + 8 * i, zero);
-  }
 }
 
 // The block's rows [0, rows) of queries, `copies` times, swizzled; 256 threads.  All loads go out before `ready` is asked for, which says that the memory is free.
@@ -473,6 +462,40 @@ __device__ __forceinline__ bool load_queries(const Params &p, const Block &w, un
   return true;
 }
 
+// A row with a NaN or an infinity: from a value that it does not see (0 times it is NaN), or its own.  The row r of the block once more, key by key, by one
+// warp: the keys that lie in the columns [first, first + size) of each tile, `columns` elements from column0 on; finished, or relative to the
+// maximum of the part that it belongs to.  Out of line: hardly ever called.
+template <typename T, int D>
+__device__ __noinline__ void once_more(const Params &p, const Block &w, int r, int first, int size, int column0, int columns, bool finish, float part_m,
+                                       float *to_part) {
+  const int lane = threadIdx.x & 31, i = token_of(p, w.row0 + r), h = w.head * p.group + w.row0 + r - i * p.group;
+  const Sight see = sight_of(p, w);
+  constexpr int E = D / 32;
+  float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 1
+  for (int t = w.k0; t < w.k1; ++t) {
+    const int key = w.key0(t), last = last_box(w.keys - key, p.box_rows), over = shift_of_last_box(w.keys - key, p.box_rows);
+#pragma unroll 1
+    for (int shifted = 0; shifted < 2; ++shifted) {
+      const int lo = shifted ? max(first - over, last) : first, hi = shifted ? first + size - over : min(first + size, last);
+      if (!shifted || last < kTile) attend_row<T, D>(p.c, p.a, see, w.b, i, h, key + lo, min(key + hi, w.keys), m, l, o);
+    }
+  }
+  const float f = l == 0.f ? 0.f : finish ? 1.f / l : exp2f(m - part_m);
+  T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i * p.a.out_token_stride + h * p.a.out_head_stride;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int d = lane * E + e;
+    const float x = f == 0.f ? 0.f : o[e] * f;
+    if (d < column0 || d >= column0 + columns) continue;
+    if (finish) out[d] = from_float<T>(x);
+    else to_part[(d >> 2) * (kBlockRows * 4) + (d & 3)] = x;
+  }
+  __syncwarp();
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
   constexpr int kRing = Ring<D>::n;
@@ -501,77 +524,48 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 
   // ---- the thread block's share of the tiles
   if (p.split) {
-    long long carry = 0;
-    if (n_pairs <= kThreads) {              // everything in one round: no need for the list
-      const Block w = tid < n_pairs ? block_of(p, tid) : Block{};
-      long long x = tid < n_pairs ? w.tiles : 0;
-      const int mine = (int)x;
+    int carry = 0;
+#pragma unroll 1
+    for (int base = 0; base < n_pairs; base += kThreads) {
+      const int pair = base + tid, mine = pair < n_pairs ? block_of(p, pair).tiles : 0;
+      int x = mine;
+#pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(~0u, x, d);
+        const int y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
       }
       if (lane == 31) sh.warp_sum[warp] = x;
       __syncthreads();
-      long long earlier = 0;
+      int earlier = 0, all = 0;
+#pragma unroll
       for (int v = 0; v < kThreads / 32; ++v) {
-        const long long s = sh.warp_sum[v];
+        const int s = sh.warp_sum[v];
         earlier += v < warp ? s : 0;
-        carry += s;
+        all += s;
       }
-      const Deal deal(carry * p.c.kv_heads, G);
-      const long long begin = deal.begin(blockIdx.x), first = (earlier + x - mine) * p.c.kv_heads;
-      if (tid == 0) sh.left = deal.begin(blockIdx.x + 1) - begin;
-      if (mine > 0 && begin >= first && begin < first + (long long)mine * p.c.kv_heads) {
-        const long long in_pair = begin - first;
-        sh.pair = tid;
-        sh.head = (int)(in_pair < 0x7FFFFFFF ? (uint32_t)in_pair / (uint32_t)mine : in_pair / mine);
-        sh.k0 = (int)(in_pair - (long long)sh.head * mine);
-      }
-    } else {
-      for (int base = 0; base < n_pairs; base += kThreads) {
-        const int pair = base + tid;
-        const long long mine = pair < n_pairs ? block_of(p, pair).tiles : 0;
-        long long x = mine;
-        for (int d = 1; d < 32; d <<= 1) {
-          const long long y = __shfl_up_sync(~0u, x, d);
-          if (lane >= d) x += y;
-        }
-        if (lane == 31) sh.warp_sum[warp] = x;
-        __syncthreads();
-        long long earlier = 0, all = 0;
-        for (int v = 0; v < kThreads / 32; ++v) {
-          const long long s = sh.warp_sum[v];
-          earlier += v < warp ? s : 0;
-          all += s;
-        }
-        if (pair < n_pairs) sh.before[pair] = carry + earlier + x - mine;
-        carry += all;
-        __syncthreads();
-      }
-      if (tid == 0) sh.before[n_pairs] = carry;
+      if (pair < n_pairs) sh.before[pair] = carry + earlier + x - mine;
+      carry += all;
       __syncthreads();
-      const Deal deal(carry * p.c.kv_heads, G);
-      const long long begin = deal.begin(blockIdx.x);
-      if (tid == 0) sh.left = deal.begin(blockIdx.x + 1) - begin;
-      for (int pair = tid; pair < n_pairs; pair += kThreads) {
-        const long long first = sh.before[pair] * p.c.kv_heads, last = sh.before[pair + 1] * p.c.kv_heads;
-        if (begin < first || begin >= last) continue;
-        const long long mine = sh.before[pair + 1] - sh.before[pair], in_pair = begin - first;
-        sh.pair = pair;
-        sh.head = (int)(in_pair / mine);
-        sh.k0 = (int)(in_pair % mine);
-      }
     }
+    if (tid == 0) sh.before[n_pairs] = carry;
     __syncthreads();
+    const Deal deal(carry * p.c.kv_heads, G);
+    const int begin = deal.begin(blockIdx.x), left = deal.begin(blockIdx.x + 1) - begin;
     if (tid == 0) {
-      int4 cut = make_int4(-1, 0, 0, 0);
-      if (sh.left > 0 && sh.k0 > 0) {       // a block of rows that an earlier thread block began
-        const Deal deal(carry * p.c.kv_heads, G);
-        const long long item = deal.begin(blockIdx.x) - sh.k0, last = item + block_of(p, sh.pair).tiles - 1;
-        const int c0 = deal.owner(item);
-        if (c0 == (int)blockIdx.x - 1) cut = make_int4(sh.pair, sh.head, c0, deal.owner(last));
-      }
-      p.cut[blockIdx.x] = cut;
+      sh.left = left;
+      if (left == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    }
+#pragma unroll 1
+    for (int pair = tid; pair < n_pairs && left > 0; pair += kThreads) {
+      const int first = sh.before[pair] * p.c.kv_heads, mine = sh.before[pair + 1] - sh.before[pair];
+      if (begin < first || begin >= first + mine * p.c.kv_heads) continue;      // (one pair of one thread)
+      const int head = (begin - first) / mine, k0 = begin - first - head * mine;
+      sh.pair = pair;
+      sh.head = head;
+      sh.k0 = k0;
+      // a block of rows that the thread block before this one began
+      const int c0 = k0 > 0 ? deal.owner(begin - k0) : -1;
+      p.cut[blockIdx.x] = k0 > 0 && c0 == (int)blockIdx.x - 1 ? make_int4(pair, head, c0, deal.owner(begin - k0 + mine - 1)) : make_int4(-1, 0, 0, 0);
     }
   }
   tmem_fence_before();
@@ -601,35 +595,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   if (warp == 10) {
     // ------------------------------------------------------------ the walk
     if (lane == 0) {
-      long long left = sh.left, item = blockIdx.x;
-      int pair = sh.pair, head = sh.head, k0 = sh.k0, known = -1;
+      int left = sh.left, pair = p.split ? sh.pair : 0, head = p.split ? sh.head : blockIdx.x, k0 = p.split ? sh.k0 : 0, known = -1;
       Block w;
-      w.rows = 0;
       for (int i = 0;; ++i) {
         bool more = false;
-        if (p.split) {
-          while (left > 0 && pair < n_pairs) {
-            if (pair != known) { w = block_of(p, pair); known = pair; }
-            if (w.tiles > 0) { more = true; break; }
-            ++pair;
-          }
-          if (more) {
-            w.head = head;
-            w.k0 = k0;
-            w.k1 = (int)min((long long)w.tiles, k0 + left);
-            left -= w.k1 - k0;
-            k0 = 0;
-            if (++head == p.c.kv_heads) { head = 0; ++pair; }
-          }
-        } else {
-          for (; item < (long long)n_pairs * p.c.kv_heads && !more; item += G) {
-            pair = (int)(item / p.c.kv_heads);
-            if (pair != known) { w = block_of(p, pair); known = pair; }
-            w.head = (int)(item - (long long)pair * p.c.kv_heads);
-            w.k1 = w.tiles;
-            more = w.tiles > 0;
-          }
+#pragma unroll 1
+        while ((!p.split || left > 0) && !more) {
+          while (head >= p.c.kv_heads) { head -= p.c.kv_heads; ++pair; }
+          if (pair >= n_pairs) break;
+          if (pair != known) w = block_of(p, pair);
+          known = pair;
+          more = w.tiles > 0;
+          w.head = head;
+          if (p.split && !more) head = p.c.kv_heads;            // to the next pair
+          else head += p.split ? 1 : G;
         }
+        w.k0 = k0;
+        w.k1 = p.split ? min(w.tiles, k0 + left) : w.tiles;
+        left -= w.k1 - k0;
+        k0 = 0;
         if (!wait(sh, sh.read + i % kBlocks, (i / kBlocks & 1) ^ 1)) break;
         if (!more) w.rows = 0;
         sh.block[i % kBlocks] = w;
@@ -675,7 +659,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         __syncwarp();
         if (lane < boxes)
           copy_box(shared_address(sh.ring[to.at]) + half * (kTile * 128) + part * box_bytes, values ? &maps.v : &maps.k, sh.full + to.at, half * 64, w.head,
-                   key & (p.c.page_size - 1), page, p.a.layer);
+                   (key & (p.c.page_size - 1)) - (key < w.keys ? max(key + p.box_rows - w.keys, 0) : 0), page, p.a.layer);
         to.step(1);
         ++filled;
         page = next; values = next_values; key = next_key;
@@ -697,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
                    v_tile = tile_descriptor(shared_address(sh.ring[0]), 1024, kTile * 128);
     const bool leader = elect_one();
     Cursor<kRing> keys = {0, 0}, vals;
-    uint32_t weights_parity[2] = {0, 0};
+    uint32_t weights_parity = 0;            // of both
     bool ok = true;
     int item = 0;
     auto arrived = [&](uint64_t *bar, uint32_t parity) { return warp_wait(sh, bar, parity); };
@@ -731,60 +715,36 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       const int n = uniform(sh.block[item % kBlocks].k1 - sh.block[item % kBlocks].k0), rows = uniform(sh.block[item % kBlocks].rows);
       block_read(item);
       if (rows == 0) break;
-      const int ahead = rows > kRows ? 1 : 2;
+      // One step after the other: O += P V of an accumulator's tile, then its next logits.  With both halves of the rows over every tile the steps are
+      // (tile, half), else the tiles; two steps come first that have logits only.
+      const bool two = rows > kRows;
+      const int ahead = two ? 1 : 2, steps = two ? 2 * n : n;
       vals = keys;
       vals.step(min(n, ahead));
       if (!(ok = arrived(&sh.queries, item & 1))) break;
       tmem_fence_after();
-      if (rows > kRows) {                   // both halves of the rows over every tile
-        if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
-        logits(0, 0, keys.at);
-        logits(1, 1, keys.at);
-        free_buffer(keys.at);
-        for (int t = 0; t < n; ++t) {
-          keys.step(2);
-          if (!(ok = arrived(sh.full + vals.at, vals.parity))) break;
-          if (!(ok = arrived(sh.weights, weights_parity[0]))) break;
-          weights_parity[0] ^= 1;
+#pragma unroll 1
+      for (int e = -2; e < steps; ++e) {
+        const int s = e & 1, t = two ? e >> 1 : e, next = t + ahead;
+        const bool first_of = !two || s == 0, last_of = !two || s == 1;         // of the tile's steps
+        if (e >= 0) {
+          if (first_of && !(ok = arrived(sh.full + vals.at, vals.parity))) break;
+          if (!(ok = arrived(sh.weights + s, weights_parity >> s & 1))) break;
+          weights_parity ^= 1u << s;
           tmem_fence_after();
-          mix(0, vals.at, t > 0);
-          if (t + 1 < n) {
-            if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
-            logits(0, 0, keys.at);
+          mix(s, vals.at, t >= ahead);
+          if (last_of) {
+            free_buffer(vals.at);
+            vals.step(step_of_values(t, n, ahead));
           }
-          if (!(ok = arrived(sh.weights + 1, weights_parity[1]))) break;
-          weights_parity[1] ^= 1;
-          tmem_fence_after();
-          mix(1, vals.at, t > 0);
-          free_buffer(vals.at);
-          if (t + 1 < n) {
-            logits(1, 1, keys.at);
-            free_buffer(keys.at);
-          }
-          vals.step(step_of_values(t, n, 1));
         }
-      } else {                              // all rows, every other tile
-        for (int t = 0; t < min(n, 2); ++t) {
-          if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
-          logits(t, 0, keys.at);
-          free_buffer(keys.at);
-          keys.step(step_of_keys(t, 2));
-        }
-        for (int t = 0; t < n && ok; ++t) {
-          const int s = t & 1;
-          if (!(ok = arrived(sh.full + vals.at, vals.parity))) break;
-          if (!(ok = arrived(sh.weights + s, s ? weights_parity[1] : weights_parity[0]))) break;
-          if (s) weights_parity[1] ^= 1; else weights_parity[0] ^= 1;
-          tmem_fence_after();
-          mix(s, vals.at, t > 1);
-          free_buffer(vals.at);
-          if (t + 2 < n) {
-            if (!(ok = arrived(sh.full + keys.at, keys.parity))) break;
-            logits(s, 0, keys.at);
+        if (next < n) {
+          if (first_of && !(ok = arrived(sh.full + keys.at, keys.parity))) break;
+          logits(s, two ? s : 0, keys.at);
+          if (last_of) {
             free_buffer(keys.at);
-            keys.step(2);
+            keys.step(step_of_keys(next, ahead));
           }
-          vals.step(step_of_values(t, n, 2));
         }
       }
       if (!ok) break;
@@ -803,10 +763,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, my_s = tmem + s * kTile + lanes, my_o = tmem + 256 + s * 128 + lanes;
     const float unit = p.a.scale * kLog2e;
     float *stage = reinterpret_cast<float *>(sh.q[0]) + warp * (D * 16);        // D * 64 bytes a warp
-    Cursor<kRing> vals_at, base = {0, 0};
     uint32_t logits_parity = 0, meet_parity = 0;
     bool ok = true;
-    int item = 0, turn = 0;                 // buffers of the ring so far
+    int item = 0;
     auto all_meet = [&] {
       barrier_arrive(&sh.meet);
       const bool met = warp_wait(sh, &sh.meet, meet_parity);
@@ -835,40 +794,30 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       {
         const Sight see = sight_of(p, w);
         const int own = see.position(node);
-        vals_at = base;
-        vals_at.step(min(n, ahead));
-        if (!two && s == 1) vals_at.step(step_of_values(0, n, ahead));
         for (int t = two ? 0 : s; t < n; t += ahead) {
           const int key = w.key0(w.k0 + t);
           const bool all = key + kTile <= see.prefix && key + kTile <= see.keys && (see.window == 0 || key > own - see.window || key + kTile <= see.sinks);
           const bool masked = !__all_sync(~0u, all);
+          const int last = last_box(see.keys - key, p.box_rows), over = shift_of_last_box(see.keys - key, p.box_rows);
           uint32_t on[4] = {~0u, ~0u, ~0u, ~0u};
           if (masked && warp_live) {        // (while the logits are on their way)
 #pragma unroll 1
             for (int i = copy_rows / 32; i > 0; --i) {
               on[3] = on[2]; on[2] = on[1]; on[1] = on[0];
-              on[0] = sight_bits(see, node, own, key + first_column + 32 * (i - 1));
+              const int c = first_column + 32 * (i - 1);
+              uint32_t word = 0;
+#pragma unroll 1
+              for (int shift = 0; shift <= over; shift += max(over, 1))         // the columns before the last box, then the box
+                word |= sight_bits(see, node, own, key + c - shift) & (shift ? ~low_bits(last + over - c) : low_bits(over ? last - c : 32));
+              on[0] = word;
             }
           }
           if (!(ok = warp_wait(sh, sh.logits + s, logits_parity))) break;
           logits_parity ^= 1;
           tmem_fence_after();
-          if (key + kTile > see.keys) {     // rows of the values that nobody wrote: their weights are 0, they must be numbers
-            if (!(ok = warp_wait(sh, sh.full + vals_at.at, vals_at.parity))) break;
-            if (key + row >= see.keys && !(two && s == 1)) {    // (the first group's are in time for both)
-#pragma unroll
-              for (int i = 0; i < D / 8; ++i)
-                *reinterpret_cast<uint4 *>(sh.ring[vals_at.at] + (i >> 3) * (kTile * 128) + row * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-            }
-            shared_writes_fence();
-          }
-          vals_at.step(step_of_values(t, n, ahead));
-          if (!two) vals_at.step(step_of_values(t + 1, n, ahead));
           __syncwarp();
           if (warp_live) {
-            if (copy_rows == 32) softmax_tile<T, D, 2>(my_s, my_o, first_column, masked, on, unit, t >= ahead, m, l);
-            else if (copy_rows == 64) softmax_tile<T, D, 4>(my_s, my_o, first_column, masked, on, unit, t >= ahead, m, l);
-            else softmax_tile<T, D, 8>(my_s, my_o, 0, masked, on, unit, t >= ahead, m, l);
+            softmax_tile<T, D>(my_s, my_o, first_column, copy_rows / 32, masked, on[0], on[1], on[2], on[3], unit, t >= ahead, m, l);
             tmem_wait_stores();
           }
           tmem_fence_before();
@@ -880,9 +829,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         break;
       }
       tmem_fence_after();
-      turn += 2 * n;
-      base.at = turn % kRing;
-      base.parity = turn / kRing & 1;
 
       // ---- what the thread block has of its rows: finished, or a part for the other launch to add up
       const bool whole = w.k0 == 0 && w.k1 == w.tiles;
@@ -893,9 +839,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         if (!(ok = all_meet())) break;
         const int lane_row = whole ? my_row : row, step = whole ? copy_rows : kRows;
         m = -INFINITY;
+#pragma unroll 1
         for (int i = lane_row; i < kRows; i += step) m = fmaxf(m, fmaxf(sh.ml[0][i].x, sh.ml[1][i].x));
         l = 0.f;
+#pragma unroll 1
         for (int i = lane_row; i < kRows; i += step)
+#pragma unroll
           for (int v = 0; v < 2; ++v) {
             const float2 e = sh.ml[v][i];
             const float f = e.x == -INFINITY ? 0.f : exp2_fast(e.x - m);
@@ -927,98 +876,65 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         }
         return fine;
       };
-      // A NaN or an infinity: from a value that the row does not see (0 times it is NaN), or its own.  The row once more, key by key: those of the
-      // tiles that lie in [first, first + size) of each; in units of the share, or relative to the part's maximum.
-      auto once_more = [&](int r, int first, int size, bool finish, float part_m, float *to_part) {
-        const int i_ = token_of(p, w.row0 + r), h_ = w.head * p.group + w.row0 + r - i_ * p.group;
-        const Sight see = sight_of(p, w);
-        constexpr int E = D / 32;
-        float m2 = -INFINITY, l2 = 0.f, o2[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) o2[e] = 0.f;
-        for (int t = w.k0; t < w.k1; ++t)
-          attend_row<T, D>(p.c, p.a, see, w.b, i_, h_, w.key0(t) + first, min(w.key0(t) + first + size, w.keys), m2, l2, o2);
-        const float f = l2 == 0.f ? 0.f : finish ? 1.f / l2 : exp2f(m2 - part_m);
-        T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + i_ * p.a.out_token_stride + h_ * p.a.out_head_stride;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int d = lane * E + e;
-          const float x = f == 0.f ? 0.f : o2[e] * f;
-          if (d < column0 || d >= column0 + columns) continue;
-          if (finish) out[d] = from_float<T>(x);
-          else to_part[(d >> 2) * (kBlockRows * 4) + (d & 3)] = x;
+      // A part: 16 bytes a lane, the rows side by side.  Finished rows go through shared memory, so that they leave in whole sectors and their copies are added
+      // up: a warp's 32 rows, 32 columns at a time, 8 vectors a row, swizzled; 4 rows leave at a time, 8 lanes a row.
+      const int place = two ? my_row : row;
+      const int rows_here = two ? 32 : copy_rows / 4, r0 = two ? my_row & ~31 : (warp & 3) * rows_here;         // that this warp writes
+      const bool own_rows = two || copy_rows == kRows;          // without copies they are its own, and leave before the next columns come
+      const float *from = two ? stage : reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);            // the warp's, the group's
+      auto write = [&](int c, const float *chunk) {             // 32 columns from c on
+#pragma unroll 2
+        for (int i = 0; i < rows_here; i += 4) {
+          const int r = r0 + i + (lane >> 3), at = two ? r & 31 : r;
+          if (r >= w.rows) break;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+          for (int a = at; a < (two ? 32 : kRows); a += two ? 32 : copy_rows) {
+            const float4 x = *reinterpret_cast<const float4 *>(chunk + (a >> 5) * (D * 16) + (a & 31) * 32 + (((lane & 7) ^ (a & 7)) << 2));
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+          }
+          const int node_ = token_of(p, w.row0 + r), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
+          T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
+          *reinterpret_cast<uint2 *>(out + c + 4 * (lane & 7)) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
         }
         __syncwarp();
       };
-
-      if (!whole) {
-        // a part: 16 bytes a lane, the rows side by side
-        const int place = two ? my_row : row;
-        float *to = p.part_o + (part * (D / 4) * kBlockRows + place) * 4;
-        bool fine = true;
-        for (int c = 0; c < columns && warp_live; c += 32) {
+      if (live && (two || (s == 0 && (!whole || row == my_row)))) {
+        if (!whole) p.part_ml[part * kBlockRows + place] = make_float2(m, l);
+        else if (p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      }
+      bool fine = true;
+#pragma unroll 1
+      for (int c = 0; c < columns; c += 32) {
+        if (warp_live) {
           float v[32];
           fine &= sums(column0 + c, v);
-#pragma unroll
-          for (int j = 0; j < 32; j += 4)
-            if (live) *reinterpret_cast<float4 *>(to + (column0 + c + j) * kBlockRows) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-          __syncwarp();
-        }
-        if (live && (two || s == 0)) p.part_ml[part * kBlockRows + place] = make_float2(m, l);
-        for (uint32_t again = __ballot_sync(~0u, live && !fine); again; again &= again - 1) {
-          const int from = __ffs(again) - 1;
-          once_more(__shfl_sync(~0u, my_row, from), two ? 0 : first_column, two ? kTile : copy_rows, false, __shfl_sync(~0u, m, from),
-                    p.part_o + (part * (D / 4) * kBlockRows + __shfl_sync(~0u, place, from)) * 4);
-        }
-      } else {
-        // Finished rows go through shared memory, so that they leave in whole sectors and their copies are added up: a warp's 32 rows, 32 columns
-        // at a time, 8 vectors a row, swizzled.  4 rows leave at a time, 8 lanes a row.
-        if (p.a.lse_dev && live && (two || (s == 0 && row == my_row)))
-          p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-        bool fine = true;
-        const int rows_here = two ? 32 : copy_rows / 4, r0 = two ? my_row & ~31 : (warp & 3) * rows_here;
-        const float *from = two ? stage : reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);
-        auto put = [&](int c, float *to) {
-          float v[32];
-          fine &= sums(c, v);
+          float *to = whole ? stage + (own_rows ? 0 : c * 32) + lane * 32 : p.part_o + ((part * (D / 4) + (column0 + c) / 4) * kBlockRows + place) * 4;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<float4 *>(to + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        };
-        auto write = [&](int c, const float *chunk) {           // 32 columns from c on
-#pragma unroll 4
-          for (int i = 0; i < rows_here; i += 4) {
-            const int r = r0 + i + (lane >> 3), at = two ? r & 31 : r;
-            if (r >= w.rows) break;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int a = at; a < (two ? 32 : kRows); a += two ? 32 : copy_rows) {
-              const float4 x = *reinterpret_cast<const float4 *>(chunk + (a >> 5) * (D * 16) + (a & 31) * 32 + (((lane & 7) ^ (a & 7)) << 2));
-              v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-            }
-            const int node_ = token_of(p, w.row0 + r), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
-            T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
-            *reinterpret_cast<uint2 *>(out + c + 4 * (lane & 7)) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
-          }
-          __syncwarp();
-        };
-        if (two) {
-          for (int c = 0; c < D && warp_live; c += 32) {
-            put(c, stage);
-            __syncwarp();
-            write(c, from);
-          }
-        } else {
-          for (int c = 0; c < columns && warp_live; c += 32) put(column0 + c, stage + c * 32);
-          const uint32_t odd = __ballot_sync(~0u, live && !fine);
-          if (lane == 0) sh.odd[warp] = odd;
-          if (copy_rows < kRows && !(ok = all_meet())) break;
-          __syncwarp();
-          for (int c = 0; c < columns; c += 32) write(column0 + c, from + c * 32);
-          fine = true;
-          for (int a = r0 + lane; a < kRows && lane < rows_here; a += copy_rows) fine &= !(sh.odd[s * 4 + (a >> 5)] >> (a & 31) & 1);
+            if (whole || live)
+              *reinterpret_cast<float4 *>(to + (whole ? (j ^ (lane & 7)) << 2 : j * (kBlockRows * 4))) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         }
-        for (uint32_t again = __ballot_sync(~0u, !fine && r0 + lane < w.rows); again; again &= again - 1)
-          once_more(r0 + __ffs(again) - 1, 0, kTile, true, 0.f, nullptr);
+        __syncwarp();
+        if (whole && own_rows) write(column0 + c, from);
+      }
+      fine |= !live;
+      if (whole && !own_rows) {
+        const uint32_t odd = __ballot_sync(~0u, !fine);
+        if (lane == 0) sh.odd[warp] = odd;
+        if (!(ok = all_meet())) break;
+#pragma unroll 1
+        for (int c = 0; c < columns; c += 32) write(column0 + c, from + c * 32);
+        fine = true;
+#pragma unroll 1
+        for (int a = r0 + lane; a < kRows && lane < rows_here; a += copy_rows) fine &= !(sh.odd[s * 4 + (a >> 5)] >> (a & 31) & 1);
+        fine |= r0 + lane >= w.rows;
+      }
+      for (uint32_t again = __ballot_sync(~0u, !fine); again; again &= again - 1) {
+        // (a lane stands for its own row of the block, or, where there were copies to add up, for one of the rows that the warp wrote)
+        const int from_lane = __ffs(again) - 1, r = __shfl_sync(~0u, whole && !own_rows ? r0 + lane : my_row, from_lane), at = __shfl_sync(~0u, place, from_lane);
+        once_more<T, D>(p, w, r, whole ? 0 : first_column, whole ? kTile : copy_rows, column0, columns, whole, __shfl_sync(~0u, m, from_lane),
+                        p.part_o + (part * (D / 4) * kBlockRows + at) * 4);
       }
       block_read(item);
     }
@@ -1201,7 +1117,8 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.group_inverse = p.group > 1 ? (uint32_t)((0x100000000ull + p.group - 1) / p.group) : 0;
   p.blocks_per_seq = (int)blocks;
   p.box_rows = p.c.page_size < kTile ? p.c.page_size : kTile;
-  p.split = blocks * p.c.batch <= kMaxPairs;
+  // (tiles of all blocks of rows are counted in 32 bits)
+  p.split = blocks * p.c.batch <= kMaxPairs && blocks * p.c.batch * p.c.kv_heads * ((int64_t)p.c.max_pages * p.c.page_size / kTile + 1) <= 0x7FFFFFFF;
   char *base = static_cast<char *>(workspace_dev);
   p.part_o = reinterpret_cast<float *>(base + at.o);
   p.part_ml = reinterpret_cast<float2 *>(base + at.ml);
