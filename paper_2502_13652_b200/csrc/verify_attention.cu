@@ -182,16 +182,19 @@ struct Deal {
 //   warp 8    issues the products: logits S = Q K^T (both from shared memory), and O += P V with P, the weights, in tensor memory in S's place
 //   warp 9    copies the tiles of keys and values, a box per page and 64 elements of a head, into a ring of buffers
 //   warp 10   walks through the thread block's share and describes the next blocks of rows to the others
-// The running maximum is only raised when a row's new one is more than 2^8 in weight above it: then O and the sum are rescaled.  Weights
-// are so at most 2^8, which both types hold.
+// The running maximum is only raised when a row's new one is more than 2^14 (bf16: 2^40) in weight above it: then O and the sum are rescaled.  Weights are
+// so at most 2^14, which f16 holds, or 2^40, of which 32 bits hold any sum; a weight's precision does not depend on its size.  (At 2^8 rows that
+// begin with a few first keys asked for a second pass in their second tile: 16 windows of 1024, 64 heads, 82 -> 102 us.)
 // Up to 32 (64) rows lie in the accumulator four times (twice), and each copy takes a quarter (half) of a tile's keys, with weights of 0
 // for the others: all warps have work then, and a tile's softmax, which is what such a block waits for, a quarter of the steps.
 
 constexpr int kSoftmaxThreads = 256, kThreads = 352;
-constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x 128 at most
-constexpr float kRaise = 8.f;
-constexpr int kProducts = 2;                // of 8 powers of two that are not taken by the special-function unit: 2 kProducts / 2
+constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x D; P in the place of S, with heads of 64 in columns of its own
+template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 14.f : 40.f;
+constexpr int kProducts = 1;                // of 8 powers of two that are not taken by the special-function unit: 2 kProducts / 2
 constexpr int kTries = 1 << 22;             // of a wait, after which the block gives up
+
+template <int D> __device__ __forceinline__ constexpr int weights_at(int s) { return D == 64 ? 384 + s * 64 : s * kTile; }
 
 template <int D> struct Ring { static constexpr int bytes = kTile * D * 2, n = D == 128 ? 5 : 10; };
 
@@ -341,7 +344,12 @@ __device__ __forceinline__ void exp2_products(float &x, float &y) {
   y = __int_as_float(__float_as_int(py) + (__float_as_int(ny) << 23));
 }
 
-// the larger one; NaN if any is
+// the largest; NaN if any is
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float x;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+  return x;
+}
 __device__ __forceinline__ float larger(float a, float b) {
   float x;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
@@ -365,55 +373,61 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
   return *reinterpret_cast<const uint32_t *>(&x);
 }
 
-// A row's softmax over `words` * 32 of a tile's logits, from column `first` on: their maximum, then the weights, 32 at a time.  Reading tensor memory twice
-// costs less than holding 128 logits, and a loop less than the same unrolled: the whole kernel has to stay in the instruction cache (at 200 KB of
-// instructions a tile with masks, which comes once per block of rows, took 5000 to 25000 cycles to be fetched).
+// A row's softmax over `words` * 32 of a tile's logits, from column `first` on.  Once a row has a maximum the weights are computed with it at once, and their
+// own maximum is taken on the way: it hardly ever asks for another one, and a tile's softmax, which the next products of its accumulator wait
+// for, is one pass.  Where the weights go where the logits lie they are held back till then.
 template <typename T, int D>
-__device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int first, int words, bool masked, uint32_t on0, uint32_t on1, uint32_t on2,
+__device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_w, uint32_t my_o, int first, int words, bool masked, uint32_t on0, uint32_t on1, uint32_t on2,
                                              uint32_t on3, float unit, bool has_sums, float &m, float &l) {
-  uint32_t y[32];
-  float top[2] = {-INFINITY, -INFINITY};
+  constexpr bool kHeld = D == 128;          // the weights go where the logits lie
+  uint32_t y[32], packed[kHeld ? kTile / 2 : 16];
+  float sum[4];
+  int again = __any_sync(~0u, m == -INFINITY);
+  for (;;) {
+    asm volatile("" : "+r"(again));         // (one copy of the code for both)
+    if (again) {
+      float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-  for (int i = 0; i < words; ++i) {
-    tmem_load32(my_s + first + 32 * i, y);
-    tmem_wait_loads();
-    mask32(masked, i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3, y);
+      for (int i = 0; i < words; ++i) {
+        __syncwarp();
+        tmem_load32(my_s + first + 32 * i, y);
+        tmem_wait_loads();
+        mask32(masked, i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3, y);
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      top[0] = larger(larger(top[0], __uint_as_float(y[j])), __uint_as_float(y[j + 1]));
-      top[1] = larger(larger(top[1], __uint_as_float(y[j + 2])), __uint_as_float(y[j + 3]));
-    }
-  }
-  const float highest = larger(top[0], top[1]);
-  if (!(highest < INFINITY)) l = NAN;       // (a logit that is none makes the row NaN, whichever way its power is taken)
-  // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
-  const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise);
-  const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
-  if (raise) { l *= factor; m = highest; }
-  if (__any_sync(~0u, raise) && has_sums) {
+        for (int j = 0; j < 32; j += 4) {
+          top[0] = largest(top[0], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
+          top[1] = largest(top[1], __uint_as_float(y[j + 2]), __uint_as_float(y[j + 3]));
+        }
+      }
+      const float highest = larger(top[0], top[1]);
+      // (m = -inf: nothing seen so far, the sums are 0 or not there yet)
+      const bool raise = highest > m && (m == -INFINITY || (highest - m) * unit > kRaise<T>);
+      const float factor = raise ? exp2_fast((m - highest) * unit) : 1.f;
+      if (raise) { l *= factor; m = highest; }
+      if (__any_sync(~0u, raise) && has_sums) {
 #pragma unroll 1
-    for (int i = 0; i < D; i += 32) {
-      tmem_load32(my_o + i, y);
-      tmem_wait_loads();
+        for (int i = 0; i < D; i += 32) {
+          tmem_load32(my_o + i, y);
+          tmem_wait_loads();
 #pragma unroll
-      for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * factor);
-      tmem_store32(my_o + i, y);
+          for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * factor);
+          tmem_store32(my_o + i, y);
+        }
+      }
     }
-  }
-  const float shift = m == -INFINITY ? 0.f : -m * unit;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    const int column = first + 32 * i;      // (words = 4: in order, so that no logits are overwritten that are still to be read)
-    uint32_t packed[16];
-    if (i < words) {
-      __syncwarp();
-      tmem_load32(my_s + column, y);
+    const float shift = m == -INFINITY ? 0.f : -m * unit;
+    float top[2] = {-INFINITY, -INFINITY};
+    sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+    __syncwarp();
+    auto word = [&](int i, uint32_t *packed) {                  // 32 logits
+      tmem_load32(my_s + first + 32 * i, y);
       tmem_wait_loads();
       mask32(masked, i == 0 ? on0 : i == 1 ? on1 : i == 2 ? on2 : on3, y);
 #pragma unroll
       for (int j = 0; j < 32; j += 4) {
         float a = __uint_as_float(y[j]), b = __uint_as_float(y[j + 1]), c = __uint_as_float(y[j + 2]), d = __uint_as_float(y[j + 3]);
+        top[0] = largest(top[0], a, b);
+        top[1] = largest(top[1], c, d);
         scale_add2(a, b, unit, shift);
         scale_add2(c, d, unit, shift);
         a = exp2_fast(a); b = exp2_fast(b);
@@ -424,14 +438,41 @@ __device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_o, int f
         packed[j / 2] = pack<T>(a, b);
         packed[j / 2 + 1] = pack<T>(c, d);
       }
-    } else {                                // the keys of the other copies
+    };
+    if (kHeld) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) packed[j] = 0;
+      for (int i = 0; i < 4; ++i) {
+        if (i < words) {
+          word(i, packed + 16 * i);
+        } else {                            // of the other copies
+#pragma unroll
+          for (int j = 0; j < 16; ++j) packed[16 * i + j] = 0;
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        if (i < words) {
+          word(i, packed);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) packed[j] = 0;
+        }
+        __syncwarp();
+        tmem_store16(my_w + ((first + 32 * i) & (kTile - 1)) / 2, packed);
+      }
     }
-    __syncwarp();
-    tmem_store16(my_s + (column & (kTile - 1)) / 2, packed);
+    const float highest = larger(top[0], top[1]);
+    if (!(highest < INFINITY)) l = NAN;     // (a logit that is none makes the row NaN, whichever way its power is taken)
+    if (again) break;
+    again = __any_sync(~0u, (highest - m) * unit > kRaise<T>);
+    if (!again) break;
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  __syncwarp();
+  if (kHeld)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tmem_store16(my_w + ((first + 32 * i) & (kTile - 1)) / 2, packed + 16 * i);
 }
 
 // The block's rows [0, rows) of queries, `copies` times, swizzled; 256 threads.  All loads go out before `ready` is asked for, which says that the memory is free.
@@ -702,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       if (leader) {
 #pragma unroll
         for (int d = 0; d < kTile / 16; ++d)
-          product_tensor(tmem + 256 + s * 128, tmem + s * kTile + d * 8, b + d * (2048 / 16), kMix, add || d > 0);
+          product_tensor(tmem + 256 + s * D, tmem + weights_at<D>(s) + d * 8, b + d * (2048 / 16), kMix, add || d > 0);
       }
       __syncwarp();
     };
@@ -760,7 +801,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   } else {
     // ------------------------------------------------------------ softmax
     const int s = warp >> 2, row = tid & 127;                   // the accumulator; the row in it = the lane of tensor memory
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21, my_s = tmem + s * kTile + lanes, my_o = tmem + 256 + s * 128 + lanes;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, my_s = tmem + s * kTile + lanes, my_o = tmem + 256 + s * D + lanes,
+                   my_w = tmem + weights_at<D>(s) + lanes;
     const float unit = p.a.scale * kLog2e;
     float *stage = reinterpret_cast<float *>(sh.q[0]) + warp * (D * 16);        // D * 64 bytes a warp
     uint32_t logits_parity = 0, meet_parity = 0;
@@ -817,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           tmem_fence_after();
           __syncwarp();
           if (warp_live) {
-            softmax_tile<T, D>(my_s, my_o, first_column, copy_rows / 32, masked, on[0], on[1], on[2], on[3], unit, t >= ahead, m, l);
+            softmax_tile<T, D>(my_s, my_w, my_o, first_column, copy_rows / 32, masked, on[0], on[1], on[2], on[3], unit, t >= ahead, m, l);
             tmem_wait_stores();
           }
           tmem_fence_before();
@@ -865,7 +907,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         __syncwarp();
         tmem_load32((two ? my_o : tmem + 256 + lanes) + c, o);
         uint32_t o1[32];
-        if (!two) tmem_load32(tmem + 384 + lanes + c, o1);
+        if (!two) tmem_load32(tmem + 256 + D + lanes + c, o1);
         tmem_wait_loads();
         bool fine = true;
 #pragma unroll
