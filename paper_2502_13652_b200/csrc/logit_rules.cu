@@ -1,10 +1,10 @@
 // Penalties, biases and grammar masks on logits rows, and the history's counts.  See include/c2t.h.
 //
-// A row is read once and written once; the arithmetic is a handful of operations on the few tokens that the text has, so the
-// pass is bound by the memory.  A thread keeps one 16-byte vector position and goes down the rows of its sequence with it: the
-// history's counts and the biases of its tokens, which all rows share, are read once and stay in registers.  What differs from row to
-// row besides the logits is the grammar's bits and the few tokens on the row's own root path; of those the block lists, once, the ones
-// that lie in its tile of the vocabulary.
+// A row is read once and written once; the arithmetic touches only the few tokens that the text or the bias table has, and the rest of a row is
+// a copy under the grammar's mask, bound by the memory.  So a block, which has a tile of the vocabulary and some rows of a sequence, first lists the
+// tile's tokens that need more than the mask, computes their logits one by one, a thread each, and keeps them in shared memory; then it copies its
+// rows, 16 bytes a thread; then it puts the computed logits over them.  (Computing before copying allows in place.  With the arithmetic in the
+// copying loop, under a branch per vector, 64 x 60 rows of 128256 bf16 took 583 us: a warp nearly always has a lane that takes it.)
 #include <cuda_bf16.h>
 
 #include "c2t_internal.h"
@@ -16,10 +16,16 @@ constexpr int kRuleThreads = 256;
 constexpr int kRuleRows = 32;               // rows of a block, at most
 constexpr int kPathMax = C2T_MAX_DEPTH + 1;
 constexpr int kRowsAtOnce = 4;
+constexpr int kTileTokens = kRuleThreads * 8;                   // of a tile, at most
+constexpr int kKept = 4096;                 // computed logits that a block keeps: at least a tile's of one row
 
 struct RuleShared {
+  float kept[kKept], path_kept[kRuleRows][kPathMax];
+  int marks;                                // tokens of the tile with a count or a bias
+  uint16_t mark[kTileTokens];               // which, from the tile's first
   int listed[kRuleRows];                    // path tokens of the row that lie in the tile
   int token[kRuleRows][kPathMax];
+  bool path_own[kRuleRows][kPathMax];       // is it a logit that the marks do not have, here for the first time?
 };
 
 template <typename T> struct Lanes;         // elements of 16 bytes
@@ -30,6 +36,9 @@ template <> struct Lanes<float> {
   }
   static __device__ __forceinline__ uint4 close(const float *x) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ uint4 choose(const uint4 &v, unsigned on) {          // -inf where a token is not allowed
+    return make_uint4(on & 1 ? v.x : 0xFF800000u, on & 2 ? v.y : 0xFF800000u, on & 4 ? v.z : 0xFF800000u, on & 8 ? v.w : 0xFF800000u);
   }
 };
 template <> struct Lanes<__nv_bfloat16> {
@@ -48,121 +57,155 @@ template <> struct Lanes<__nv_bfloat16> {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  static __device__ __forceinline__ uint4 choose(const uint4 &v, unsigned on) {
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    unsigned y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned lo = on >> (2 * i) & 1 ? w[i] : 0xFF80u, hi = on >> (2 * i + 1) & 1 ? w[i] : 0xFF800000u;
+      y[i] = __byte_perm(lo, hi, 0x7610);
+    }
+    return make_uint4(y[0], y[1], y[2], y[3]);
+  }
 };
 
-// 16 bytes of a row; at the row's end, where a vector would reach behind it, element by element
-template <typename T>
-__device__ __forceinline__ uint4 load_vector(const T *row, int v0, int V) {
-  if (v0 + Lanes<T>::n <= V) return *reinterpret_cast<const uint4 *>(row + v0);
-  uint4 x = make_uint4(0, 0, 0, 0);
-  T *e = reinterpret_cast<T *>(&x);
-#pragma unroll
-  for (int i = 0; i < Lanes<T>::n; ++i)
-    if (v0 + i < V) e[i] = row[v0 + i];
-  return x;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_vector(T *row, int v0, int V, uint4 x) {
-  if (v0 + Lanes<T>::n <= V) {
-    *reinterpret_cast<uint4 *>(row + v0) = x;
-    return;
-  }
-  const T *e = reinterpret_cast<const T *>(&x);
-#pragma unroll
-  for (int i = 0; i < Lanes<T>::n; ++i)
-    if (v0 + i < V) row[v0 + i] = e[i];
-}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float *to, float x) { *to = x; }
+__device__ __forceinline__ void from_float(__nv_bfloat16 *to, float x) { *to = __float2bfloat16_rn(x); }
 
 // Grid (tiles of kRuleThreads vectors, groups of rows, B).  Dynamic shared memory: 2 N ints for the sequence's nodes.
 template <typename T>
-__global__ void __launch_bounds__(kRuleThreads) penalize_kernel(c2t_logit_rules a, int rows_per_block) {
+__global__ void __launch_bounds__(kRuleThreads, 4) penalize_kernel(const __grid_constant__ c2t_logit_rules a, int rows_per_block) {
   chain_enter();
   constexpr int n = Lanes<T>::n;
   __shared__ RuleShared sh;
   extern __shared__ int nodes[];
-  const int b = blockIdx.z, V = a.vocab;
-  const int r0 = blockIdx.y * rows_per_block;
+  const int b = blockIdx.z, V = a.vocab, r0 = blockIdx.y * rows_per_block;
   int r1 = min(r0 + rows_per_block, a.rows);
   if (a.n_rows_dev) r1 = min(r1, a.n_rows_dev[b]);
   if (r0 >= r1) return;
-  const int tile0 = blockIdx.x * kRuleThreads * n, v0 = tile0 + threadIdx.x * n;
-  const bool live = v0 < V;
+  const int rows = r1 - r0, tile0 = blockIdx.x * kRuleThreads * n, tile1 = min(tile0 + kRuleThreads * n, V), v0 = tile0 + threadIdx.x * n;
+  const int32_t *counts = a.counts_dev ? a.counts_dev + b * a.counts_stride : nullptr;
+  const float *bias = a.bias_dev ? a.bias_dev + b * a.bias_stride : nullptr;
+  const T *in = static_cast<const T *>(a.in_dev) + b * a.in_seq_stride;
+  T *out = static_cast<T *>(a.out_dev) + b * a.out_seq_stride;
+  const uint32_t *allowed = a.allowed_dev ? a.allowed_dev + b * a.allowed_seq_stride : nullptr;
+  auto count_of = [&](int v) { return counts ? max(counts[v], 0) : 0; };
+  auto bias_of = [&](int v) { return bias ? bias[v] : 0.f; };
 
-  // what the rows share
-  float count[n], bias[n];
-  bool seen = false;
-#pragma unroll
-  for (int i = 0; i < n; ++i) count[i] = bias[i] = 0.f;
-  if (live && a.counts_dev) {
-    const int32_t *c = a.counts_dev + b * a.counts_stride + v0;
-#pragma unroll
-    for (int i = 0; i < n; ++i)
-      if (v0 + i < V) { count[i] = (float)max(c[i], 0); seen |= count[i] > 0.f; }
-  }
-  if (live && a.bias_dev) {
-    const float *s = a.bias_dev + b * a.bias_stride + v0;
-#pragma unroll
-    for (int i = 0; i < n; ++i)
-      if (v0 + i < V) bias[i] = s[i];
-  }
-  const float rep = a.repetition_dev ? a.repetition_dev[b] : 1.f, freq = a.frequency_dev ? a.frequency_dev[b] : 0.f,
-              pres = a.presence_dev ? a.presence_dev[b] : 0.f;
-
-  // the rows' own tokens
-  const int rows = r1 - r0;
+  // ---- the tile's tokens in the history or the bias table, and the rows' own
+  if (threadIdx.x == 0) sh.marks = 0;
   if (threadIdx.x < rows) sh.listed[threadIdx.x] = 0;
   if (a.node_token_dev) {
-    int *token = nodes, *parent = nodes + a.nodes;
     for (int i = threadIdx.x; i < a.nodes; i += kRuleThreads) {
-      token[i] = a.node_token_dev[(long long)b * a.nodes + i];
-      parent[i] = a.node_parent_dev[(long long)b * a.nodes + i];
+      nodes[i] = a.node_token_dev[(long long)b * a.nodes + i];
+      nodes[a.nodes + i] = a.node_parent_dev[(long long)b * a.nodes + i];
     }
-    __syncthreads();
-    if (threadIdx.x < rows) {
-      const int r = r0 + threadIdx.x;
-      int node = a.row_node_dev ? a.row_node_dev[(long long)b * a.rows + r] : r, found = 0;
-      for (int d = 0; d < kPathMax && node >= 0 && node < a.nodes; ++d) {
-        const int t = token[node];
-        if (t >= tile0 && t < tile0 + kRuleThreads * n && t < V) sh.token[threadIdx.x][found++] = t;
-        node = parent[node];
-      }
-      sh.listed[threadIdx.x] = found;
+  }
+  unsigned marked = 0;
+  if (counts || bias) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) {           // (side by side in a warp: whole sectors)
+      const int v = tile0 + i * kRuleThreads + threadIdx.x;
+      if (v < tile1) marked |= (count_of(v) > 0 || bias_of(v) != 0.f ? 1u : 0u) << i;
     }
   }
   __syncthreads();
-  if (!live) return;
+  if (marked) {
+    int at = atomicAdd(&sh.marks, __popc(marked));
+    for (; marked; marked &= marked - 1) sh.mark[at++] = (uint16_t)((__ffs(marked) - 1) * kRuleThreads + threadIdx.x);
+  }
+  if (a.node_token_dev && threadIdx.x < rows) {
+    const int r = r0 + threadIdx.x;
+    int node = a.row_node_dev ? a.row_node_dev[(long long)b * a.rows + r] : r, found = 0;
+    for (int d = 0; d < kPathMax && node >= 0 && node < a.nodes; ++d) {
+      const int t = nodes[node];
+      if (t >= tile0 && t < tile1) sh.token[threadIdx.x][found++] = t;
+      node = nodes[a.nodes + node];
+    }
+    sh.listed[threadIdx.x] = found;
+  }
+  __syncthreads();
 
-  const T *in = static_cast<const T *>(a.in_dev) + b * a.in_seq_stride;
-  T *out = static_cast<T *>(a.out_dev) + b * a.out_seq_stride;
-  const uint32_t *allowed = a.allowed_dev ? a.allowed_dev + b * a.allowed_seq_stride + (v0 >> 5) : nullptr;
-  for (int r = r0; r < r1; r += kRowsAtOnce) {
-    uint4 raw[kRowsAtOnce];
-    unsigned on[kRowsAtOnce];
-#pragma unroll
-    for (int u = 0; u < kRowsAtOnce; ++u) {
-      if (r + u >= r1) break;
-      raw[u] = load_vector(in + (r + u) * a.in_row_stride, v0, V);
-      on[u] = allowed ? allowed[(r + u) * a.allowed_row_stride] >> (v0 & 31) : ~0u;
+  // ---- their logits
+  auto ruled = [&](int row, int v) {        // row r0 + row, token v
+    int c = count_of(v);
+#pragma unroll 1
+    for (int e = 0; e < sh.listed[row]; ++e) c += sh.token[row][e] == v;
+    float x = to_float(in[(r0 + row) * a.in_row_stride + v]);
+    if (c > 0) {
+      const float rep = a.repetition_dev ? a.repetition_dev[b] : 1.f, freq = a.frequency_dev ? a.frequency_dev[b] : 0.f,
+                  pres = a.presence_dev ? a.presence_dev[b] : 0.f;
+      x = (x > 0.f ? x / rep : x * rep) - freq * (float)c - pres;
     }
+    const float y = bias_of(v);
+    if (y != 0.f) x += y;
+    return allowed && !(allowed[(r0 + row) * a.allowed_row_stride + (v >> 5)] >> (v & 31) & 1) ? -INFINITY : x;
+  };
+  if (a.node_token_dev) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < rows * kPathMax; i += kRuleThreads) {
+      const int row = i / kPathMax, e = i - row * kPathMax;
+      if (e >= sh.listed[row]) continue;
+      const int v = sh.token[row][e];
+      bool own = count_of(v) == 0 && bias_of(v) == 0.f;
+      for (int f = 0; f < e; ++f) own &= sh.token[row][f] != v;
+      sh.path_own[row][e] = own;
+      if (own) sh.path_kept[row][e] = ruled(row, v);
+    }
+  }
+  const int marks = sh.marks, batch = marks == 0 ? rows : min(rows, kKept / marks);
+#pragma unroll 1
+  for (int first = 0; first < rows; first += batch) {
+    const int size = min(batch, rows - first);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < size * marks; i += kRuleThreads) {
+      const int row = i / marks;
+      sh.kept[i] = ruled(first + row, tile0 + sh.mark[i - row * marks]);
+    }
+    __syncthreads();                        // (the rows' path logits are kept too by now: nothing has been written yet)
+
+    // ---- the rows, under the grammar's mask
+    const int last = r0 + first + size;
+    if (v0 + n <= V) {
+#pragma unroll 1
+      for (int r = r0 + first; r < last; r += kRowsAtOnce) {
+        uint4 raw[kRowsAtOnce];
+        unsigned on[kRowsAtOnce];
 #pragma unroll
-    for (int u = 0; u < kRowsAtOnce; ++u) {
-      if (r + u >= r1) break;
-      float x[n];
-      Lanes<T>::open(raw[u], x);
-      const int listed = sh.listed[r + u - r0];
-      if (seen || listed) {
-#pragma unroll
-        for (int i = 0; i < n; ++i) {
-          float c = count[i];
-          for (int e = 0; e < listed; ++e) c += sh.token[r + u - r0][e] == v0 + i ? 1.f : 0.f;
-          if (c > 0.f) x[i] = (x[i] > 0.f ? x[i] / rep : x[i] * rep) - freq * c - pres;
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+          const int row = min(r + u, last - 1);
+          raw[u] = __ldcs(reinterpret_cast<const uint4 *>(in + row * a.in_row_stride + v0));
+          on[u] = allowed ? allowed[row * a.allowed_row_stride + (v0 >> 5)] >> (v0 & 31) : ~0u;
         }
-      }
 #pragma unroll
-      for (int i = 0; i < n; ++i) x[i] = on[u] >> i & 1 ? x[i] + bias[i] : -INFINITY;
-      store_vector(out + (r + u) * a.out_row_stride, v0, V, Lanes<T>::close(x));
+        for (int u = 0; u < kRowsAtOnce; ++u)
+          if (r + u < last) __stcs(reinterpret_cast<uint4 *>(out + (r + u) * a.out_row_stride + v0), Lanes<T>::choose(raw[u], on[u]));
+      }
+    } else {                                // the vector that reaches over the rows' end
+#pragma unroll 1
+      for (int i = 0; i < size * (V - v0); ++i) {
+        const int r = r0 + first + i / (V - v0), v = v0 + i % (V - v0);
+        const bool on = !allowed || (allowed[r * a.allowed_row_stride + (v >> 5)] >> (v & 31) & 1);
+        from_float(out + r * a.out_row_stride + v, on ? to_float(in[r * a.in_row_stride + v]) : -INFINITY);
+      }
     }
+    __syncthreads();
+
+    // ---- and over them what was computed
+#pragma unroll 1
+    for (int i = threadIdx.x; i < size * marks; i += kRuleThreads) {
+      const int row = i / marks;
+      from_float(out + (r0 + first + row) * a.out_row_stride + tile0 + sh.mark[i - row * marks], sh.kept[i]);
+    }
+    if (a.node_token_dev)
+#pragma unroll 1
+      for (int i = threadIdx.x; i < size * kPathMax; i += kRuleThreads) {
+        const int row = first + i / kPathMax, e = i % kPathMax;
+        if (e < sh.listed[row] && sh.path_own[row][e]) from_float(out + (r0 + row) * a.out_row_stride + sh.token[row][e], sh.path_kept[row][e]);
+      }
+    __syncthreads();
   }
 }
 
