@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kRuleThreads = 256;
 constexpr int kRuleRows = 32;               // rows of a block, at most
+constexpr int kRuleBlocks = 6;              // of a multiprocessor
 constexpr int kPathMax = C2T_MAX_DEPTH + 1;
 constexpr int kRowsAtOnce = 4;
 constexpr int kTileTokens = kRuleThreads * 8;                   // of a tile, at most
@@ -74,18 +75,19 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 __device__ __forceinline__ void from_float(float *to, float x) { *to = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16 *to, float x) { *to = __float2bfloat16_rn(x); }
 
-// Grid (tiles of kRuleThreads vectors, groups of rows, B).  Dynamic shared memory: 2 N ints for the sequence's nodes.
+// Grid (B, groups of rows, tiles of kRuleThreads vectors): the first tiles, with the frequent tokens and the most arithmetic, of all sequences
+// begin first.  Dynamic shared memory: 2 N ints for the sequence's nodes.
 template <typename T>
-__global__ void __launch_bounds__(kRuleThreads, 4) penalize_kernel(const __grid_constant__ c2t_logit_rules a, int rows_per_block) {
+__global__ void __launch_bounds__(kRuleThreads, kRuleBlocks) penalize_kernel(const __grid_constant__ c2t_logit_rules a, int rows_per_block) {
   chain_enter();
   constexpr int n = Lanes<T>::n;
   __shared__ RuleShared sh;
   extern __shared__ int nodes[];
-  const int b = blockIdx.z, V = a.vocab, r0 = blockIdx.y * rows_per_block;
+  const int b = blockIdx.x, V = a.vocab, r0 = blockIdx.y * rows_per_block;
   int r1 = min(r0 + rows_per_block, a.rows);
   if (a.n_rows_dev) r1 = min(r1, a.n_rows_dev[b]);
   if (r0 >= r1) return;
-  const int rows = r1 - r0, tile0 = blockIdx.x * kRuleThreads * n, tile1 = min(tile0 + kRuleThreads * n, V), v0 = tile0 + threadIdx.x * n;
+  const int rows = r1 - r0, tile0 = blockIdx.z * kRuleThreads * n, tile1 = min(tile0 + kRuleThreads * n, V), v0 = tile0 + threadIdx.x * n;
   const int32_t *counts = a.counts_dev ? a.counts_dev + b * a.counts_stride : nullptr;
   const float *bias = a.bias_dev ? a.bias_dev + b * a.bias_stride : nullptr;
   const T *in = static_cast<const T *>(a.in_dev) + b * a.in_seq_stride;
@@ -129,19 +131,15 @@ __global__ void __launch_bounds__(kRuleThreads, 4) penalize_kernel(const __grid_
   __syncthreads();
 
   // ---- their logits
-  auto ruled = [&](int row, int v) {        // row r0 + row, token v
-    int c = count_of(v);
+  const float rep = a.repetition_dev ? a.repetition_dev[b] : 1.f, freq = a.frequency_dev ? a.frequency_dev[b] : 0.f,
+              pres = a.presence_dev ? a.presence_dev[b] : 0.f;
+  auto is_on = [&](int row, int v) { return !allowed || (allowed[(r0 + row) * a.allowed_row_stride + (v >> 5)] >> (v & 31) & 1); };
+  auto ruled = [&](int row, int v, int c, float y, float x, bool on) {          // of row r0 + row, token v: its count and bias; its logit
 #pragma unroll 1
     for (int e = 0; e < sh.listed[row]; ++e) c += sh.token[row][e] == v;
-    float x = to_float(in[(r0 + row) * a.in_row_stride + v]);
-    if (c > 0) {
-      const float rep = a.repetition_dev ? a.repetition_dev[b] : 1.f, freq = a.frequency_dev ? a.frequency_dev[b] : 0.f,
-                  pres = a.presence_dev ? a.presence_dev[b] : 0.f;
-      x = (x > 0.f ? x / rep : x * rep) - freq * (float)c - pres;
-    }
-    const float y = bias_of(v);
+    if (c > 0) x = (x > 0.f ? x / rep : x * rep) - freq * (float)c - pres;
     if (y != 0.f) x += y;
-    return allowed && !(allowed[(r0 + row) * a.allowed_row_stride + (v >> 5)] >> (v & 31) & 1) ? -INFINITY : x;
+    return on ? x : -INFINITY;
   };
   if (a.node_token_dev) {
 #pragma unroll 1
@@ -152,17 +150,33 @@ __global__ void __launch_bounds__(kRuleThreads, 4) penalize_kernel(const __grid_
       bool own = count_of(v) == 0 && bias_of(v) == 0.f;
       for (int f = 0; f < e; ++f) own &= sh.token[row][f] != v;
       sh.path_own[row][e] = own;
-      if (own) sh.path_kept[row][e] = ruled(row, v);
+      if (own) sh.path_kept[row][e] = ruled(row, v, 0, 0.f, to_float(in[(r0 + row) * a.in_row_stride + v]), is_on(row, v));
     }
   }
   const int marks = sh.marks, batch = marks == 0 ? rows : min(rows, kKept / marks);
 #pragma unroll 1
   for (int first = 0; first < rows; first += batch) {
     const int size = min(batch, rows - first);
+    // a thread has a mark, and every so many-th row: what it loads for its rows goes out together
+    const int groups = marks > 0 ? max(kRuleThreads / marks, 1) : 1, group = marks > 0 ? threadIdx.x / marks : 0;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < size * marks; i += kRuleThreads) {
-      const int row = i / marks;
-      sh.kept[i] = ruled(first + row, tile0 + sh.mark[i - row * marks]);
+    for (int k = groups > 1 ? threadIdx.x - group * marks : threadIdx.x; k < marks && (groups == 1 || group < groups); k += kRuleThreads) {
+      const int v = tile0 + sh.mark[k], c = count_of(v);
+      const float y = bias_of(v);
+#pragma unroll 1
+      for (int row = groups > 1 ? group : 0; row < size; row += kRowsAtOnce * groups) {
+        float x[kRowsAtOnce];
+        bool on[kRowsAtOnce];
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+          const int r = first + min(row + u * groups, size - 1);
+          x[u] = to_float(in[(r0 + r) * a.in_row_stride + v]);
+          on[u] = is_on(r, v);
+        }
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u)
+          if (row + u * groups < size) sh.kept[(row + u * groups) * marks + k] = ruled(first + row + u * groups, v, c, y, x[u], on[u]);
+      }
     }
     __syncthreads();                        // (the rows' path logits are kept too by now: nothing has been written yet)
 
@@ -176,7 +190,7 @@ __global__ void __launch_bounds__(kRuleThreads, 4) penalize_kernel(const __grid_
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u) {
           const int row = min(r + u, last - 1);
-          raw[u] = __ldcs(reinterpret_cast<const uint4 *>(in + row * a.in_row_stride + v0));
+          raw[u] = *reinterpret_cast<const uint4 *>(in + row * a.in_row_stride + v0);
           on[u] = allowed ? allowed[row * a.allowed_row_stride + (v0 >> 5)] >> (v0 & 31) : ~0u;
         }
 #pragma unroll
@@ -253,14 +267,19 @@ int c2t_penalize_logits(const c2t_logit_rules *rules, void *stream) {
   if (odd(a.in_dev, a.in_seq_stride, a.in_row_stride) || odd(a.out_dev, a.out_seq_stride, a.out_row_stride)) return C2T_EALIGN;
 
   const int tiles = (a.vocab + kRuleThreads * (16 / esz) - 1) / (kRuleThreads * (16 / esz));
-  const int rows_per_block = a.rows < kRuleRows ? a.rows : kRuleRows;
+  // As many rows a block as leave the chip several rounds of blocks: 64 x 60 rows of 128256 bf16 take 374 us with 32 rows a block, 389 with 16, 504 with 8;
+  // 8 x 60 rows of 32000 take 59, 36, 24.
+  int sms = 0, device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return launched(cudaErrorUnknown);
+  int rows_per_block = kRuleRows;
+  while (rows_per_block > 8 && (int64_t)tiles * ((a.rows + rows_per_block - 1) / rows_per_block) * a.batch < 4ll * kRuleBlocks * sms) rows_per_block /= 2;
   const int groups = (a.rows + rows_per_block - 1) / rows_per_block;
-  if (groups > 65535) return C2T_ERANGE;
+  if (groups > 65535 || tiles > 65535) return C2T_ERANGE;
   const size_t smem = a.node_token_dev ? 2 * sizeof(int) * (size_t)a.nodes : 0;
   void (*kernel)(c2t_logit_rules, int) = a.dtype == C2T_BF16 ? penalize_kernel<__nv_bfloat16> : penalize_kernel<float>;
   if (smem > 32768 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(int) * C2T_MAX_TREE) != cudaSuccess)
     return launched(cudaErrorUnknown);
-  return launched(launch_chained(kernel, dim3(tiles, groups, a.batch), dim3(kRuleThreads), smem, (cudaStream_t)stream, a, rows_per_block));
+  return launched(launch_chained(kernel, dim3(a.batch, groups, tiles), dim3(kRuleThreads), smem, (cudaStream_t)stream, a, rows_per_block));
 }
 
 int c2t_count_tokens(int32_t *counts_dev, int64_t counts_stride, int32_t batch, int32_t vocab, const int32_t *tokens_dev,
