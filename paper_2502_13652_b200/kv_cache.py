@@ -6,11 +6,12 @@ device unless a stream is given, and nothing synchronises.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import torch
 
-from .binding import BF16, EINVAL, F32, _check, _dp, _stream, lib
+from .binding import BF16, EINVAL, F32, _check, _stream, lib
 
 F16 = 2
 ST_NO_PAGE, ST_BAD_PAGE = 32, 64
@@ -66,12 +67,32 @@ def _calls() -> C.CDLL:
     return L
 
 
-def _ints(t: Optional[torch.Tensor], n: int, device) -> Optional[int]:
-    """Pointer of a contiguous int32 tensor of n elements on `device`."""
+# The calls are short on the device, so their arguments are marshalled with as few steps as the checks allow: the structures of a call are
+# packed in one step (native alignment gives C's layout; a test compares it with the ctypes structures above).
+_ATTENTION = struct.Struct("@iiiPPqqqqqqPPPPiPiif")
+_RULES = struct.Struct("@iiiiPPqqqqPPqPPPPqPqqiPPP")
+_int32, _float32, _int64 = torch.int32, torch.float32, torch.int64
+
+
+def _ints(t: Optional[torch.Tensor], n: int, device: int) -> int:
+    """Pointer of a contiguous int32 tensor of n elements on CUDA device `device`; 0 for None."""
     if t is None:
-        return None
-    assert t.dtype == torch.int32 and t.device == device and t.is_contiguous() and t.numel() == n
+        return 0
+    assert t.dtype is _int32 and t.get_device() == device and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
+
+
+def _device_call(device: int, call, *args) -> int:
+    """call(*args) with `device` current."""
+    if torch._C._cuda_getDevice() == device:
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
+
+
+def _stream_on(device: int, stream) -> int:
+    """Handle of a stream, of the device's current one by default."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 class KVCache:
@@ -91,14 +112,17 @@ class KVCache:
         assert table.dim() == 2
         self.B, self.max_pages = table.shape
         self.device = k.device
+        self._dev = k.get_device()
         self.k, self.v, self.table, self.held, self.refs = k, v, table, held, refs
         self.status = torch.zeros(self.B, dtype=torch.int32, device=self.device)
         self._c = c2t_cache(BF16 if k.dtype == torch.bfloat16 else F16, self.B, self.layers, self.kv_heads, self.head_dim,
                             self.page_size, self.n_pages, self.max_pages, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                            k.stride(2), k.stride(3), _ints(table, self.B * self.max_pages, self.device),
-                            _ints(held, self.B, self.device), _ints(refs, self.n_pages, self.device), self.status.data_ptr())
+                            k.stride(2), k.stride(3), _ints(table, self.B * self.max_pages, self._dev), _ints(held, self.B, self._dev),
+                            _ints(refs, self.n_pages, self._dev), self.status.data_ptr())
         self._ref = C.byref(self._c)
         self._calls = _calls()
+        self._attention = C.create_string_buffer(_ATTENTION.size)
+        self._attention_at = C.cast(self._attention, C.POINTER(c2t_attention))
         self.q_heads, self.max_queries, self.workspace, self._workspace = q_heads, max_queries, None, (None, 0)
         if q_heads:
             nbytes = self._calls.c2t_verify_attention_workspace_bytes(self._ref, q_heads, max_queries)
@@ -114,54 +138,70 @@ class KVCache:
         return torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.zeros(n_pages, **i32)
 
     def _call(self, name: str, *args, stream=None) -> None:
-        with torch.cuda.device(self.device):
-            _check(getattr(self._calls, name)(self._ref, *args, _stream(stream)), name)
+        rc = _device_call(self._dev, getattr(self._calls, name), self._ref, *args, _stream_on(self._dev, stream))
+        if rc:
+            _check(rc, name)
 
     def c2t_cache_reserve(self, length: torch.Tensor, stream=None) -> None:
-        self._call("c2t_cache_reserve", _ints(length, self.B, self.device), stream=stream)
+        self._call("c2t_cache_reserve", _ints(length, self.B, self._dev), stream=stream)
 
     def c2t_cache_release(self, keep: torch.Tensor, stream=None) -> None:
-        self._call("c2t_cache_release", _ints(keep, self.B, self.device), stream=stream)
+        self._call("c2t_cache_release", _ints(keep, self.B, self._dev), stream=stream)
 
     def c2t_cache_fork(self, src: torch.Tensor, length: torch.Tensor, forked: torch.Tensor, stream=None) -> None:
-        self._call("c2t_cache_fork", *(_ints(t, self.B, self.device) for t in (src, length, forked)), stream=stream)
+        B, dev = self.B, self._dev
+        self._call("c2t_cache_fork", _ints(src, B, dev), _ints(length, B, dev), _ints(forked, B, dev), stream=stream)
 
     def c2t_cache_append(self, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, start: torch.Tensor, count: torch.Tensor,
                          stream=None) -> None:
         """k_new, v_new: [B, max_new, kv_heads, head_dim] of the cache's dtype, equal strides, last dimension contiguous."""
-        assert k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.stride() == v_new.stride()
-        assert k_new.dtype == v_new.dtype == self.k.dtype and k_new.device == v_new.device == self.device and k_new.stride(3) == 1
-        assert k_new.shape[0] == self.B and k_new.shape[2] == self.kv_heads and k_new.shape[3] == self.head_dim
-        self._call("c2t_cache_append", layer, k_new.data_ptr(), v_new.data_ptr(), k_new.shape[1], *k_new.stride()[:3],
-                   _ints(start, self.B, self.device), _ints(count, self.B, self.device), stream=stream)
+        B, dev = self.B, self._dev
+        shape, strides = k_new.shape, k_new.stride()
+        assert shape == v_new.shape and strides == v_new.stride() and k_new.dtype is v_new.dtype is self.k.dtype
+        assert len(shape) == 4 and k_new.get_device() == v_new.get_device() == dev and strides[3] == 1
+        assert shape[0] == B and shape[2] == self.kv_heads and shape[3] == self.head_dim
+        self._call("c2t_cache_append", layer, k_new.data_ptr(), v_new.data_ptr(), shape[1], strides[0], strides[1], strides[2],
+                   _ints(start, B, dev), _ints(count, B, dev), stream=stream)
 
     def c2t_cache_compact(self, prefix_len: torch.Tensor, accept_len: torch.Tensor, path: torch.Tensor,
                           new_len: Optional[torch.Tensor] = None, stream=None) -> None:
         """path: [B, D + 1] as c2t_accept writes it."""
+        B, dev = self.B, self._dev
         assert path.dim() == 2
-        self._call("c2t_cache_compact", _ints(prefix_len, self.B, self.device), _ints(accept_len, self.B, self.device),
-                   _ints(path, self.B * path.shape[1], self.device), path.shape[1], _ints(new_len, self.B, self.device), stream=stream)
+        width = path.shape[1]
+        self._call("c2t_cache_compact", _ints(prefix_len, B, dev), _ints(accept_len, B, dev), _ints(path, B * width, dev), width,
+                   _ints(new_len, B, dev), stream=stream)
 
     def c2t_verify_attention(self, layer: int, q: torch.Tensor, out: torch.Tensor, n_queries: torch.Tensor, prefix_len: torch.Tensor,
                              mask_bits: Optional[torch.Tensor] = None, position_ids: Optional[torch.Tensor] = None, window: int = 0,
                              sinks: int = 0, scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, stream=None) -> None:
         """q, out: [B, Nq, q_heads, head_dim] of the cache's dtype, last dimension contiguous; mask_bits: [B, Nq, W] int64 (the raw
         bits), None: causal; position_ids: [B, Nq] int32; lse: [B, Nq, q_heads] float32.  scale defaults to head_dim ** -0.5."""
-        assert q.dim() == 4 and q.shape == out.shape and q.dtype == out.dtype == self.k.dtype and q.device == out.device == self.device
-        assert q.shape[0] == self.B and q.shape[3] == self.head_dim and q.stride(3) == out.stride(3) == 1
-        B, Nq, heads, _ = q.shape
-        words = 0
+        B, dev = self.B, self._dev
+        shape, qs, os = q.shape, q.stride(), out.stride()
+        assert len(shape) == 4 and shape == out.shape and q.dtype is out.dtype is self.k.dtype and q.get_device() == out.get_device() == dev
+        assert shape[0] == B and shape[3] == self.head_dim and qs[3] == os[3] == 1
+        Nq, heads = shape[1], shape[2]
+        words = bits = 0
         if mask_bits is not None:
-            assert mask_bits.dtype == torch.int64 and mask_bits.device == self.device and mask_bits.is_contiguous()
-            assert mask_bits.dim() == 3 and mask_bits.shape[:2] == (B, Nq)
-            words = mask_bits.shape[2]
+            assert mask_bits.dtype is _int64 and mask_bits.get_device() == dev and mask_bits.is_contiguous()
+            assert mask_bits.dim() == 3 and mask_bits.shape[0] == B and mask_bits.shape[1] == Nq
+            bits, words = mask_bits.data_ptr(), mask_bits.shape[2]
+        lse_at = 0
         if lse is not None:
-            assert lse.dtype == torch.float32 and lse.device == self.device and lse.is_contiguous() and lse.shape == (B, Nq, heads)
-        a = c2t_attention(layer, heads, Nq, q.data_ptr(), out.data_ptr(), *q.stride()[:3], *out.stride()[:3], _dp(lse),
-                          _ints(n_queries, B, self.device), _ints(prefix_len, B, self.device), _dp(mask_bits), words,
-                          _ints(position_ids, B * Nq, self.device), window, sinks,
-                          self.head_dim ** -0.5 if scale is None else scale)
-        self._call("c2t_verify_attention", C.byref(a), *self._workspace, stream=stream)
+            assert lse.dtype is _float32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == (B, Nq, heads)
+            lse_at = lse.data_ptr()
+        _ATTENTION.pack_into(self._attention, 0, layer, heads, Nq, q.data_ptr(), out.data_ptr(), qs[0], qs[1], qs[2], os[0], os[1], os[2],
+                             lse_at, _ints(n_queries, B, dev), _ints(prefix_len, B, dev), bits, words, _ints(position_ids, B * Nq, dev),
+                             window, sinks, self.head_dim ** -0.5 if scale is None else scale)
+        self._call("c2t_verify_attention", self._attention_at, *self._workspace, stream=stream)
+
+
+def _floats(t: Optional[torch.Tensor], n: int, device: int) -> int:
+    if t is None:
+        return 0
+    assert t.dtype is _float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
 
 
 def c2t_penalize_logits(logits: torch.Tensor, out: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
@@ -173,45 +213,47 @@ def c2t_penalize_logits(logits: torch.Tensor, out: torch.Tensor, n_rows: Optiona
     """logits, out: [B, rows, V] CUDA tensors, float32 or bfloat16, last dimension contiguous (the same one for in place); counts: [B, V]
     int32; repetition, frequency, presence: [B] float32; bias: [V] or [B, V] float32; allowed: [B, rows, words] or [B, words] int32 (raw
     bits, the latter for all rows of a sequence); node_token, node_parent: [B, N] int32; row_node: [B, rows] int32."""
-    dev = logits.device
-    assert logits.is_cuda and logits.dim() == 3 and logits.shape == out.shape and logits.dtype == out.dtype and out.device == dev
-    assert logits.dtype in (torch.bfloat16, torch.float32) and logits.stride(2) == 1 and out.stride(2) == 1
-    B, R, V = logits.shape
-    for t in (repetition, frequency, presence):
-        assert t is None or (t.dtype == torch.float32 and t.device == dev and t.is_contiguous() and t.numel() == B)
+    dev = logits.get_device()
+    shape, ins, outs, dtype = logits.shape, logits.stride(), out.stride(), logits.dtype
+    assert logits.is_cuda and len(shape) == 3 and shape == out.shape and dtype is out.dtype and out.get_device() == dev
+    assert (dtype is torch.bfloat16 or dtype is _float32) and ins[2] == 1 and outs[2] == 1
+    B, R, V = shape
+    counts_at = counts_stride = bias_at = bias_stride = allowed_at = allowed_seq = allowed_row = nodes = 0
     if counts is not None:
-        assert counts.dtype == torch.int32 and counts.device == dev and counts.shape == (B, V) and counts.stride(1) == 1
+        assert counts.dtype is _int32 and counts.get_device() == dev and counts.shape == (B, V) and counts.stride(1) == 1
+        counts_at, counts_stride = counts.data_ptr(), counts.stride(0)
     if bias is not None:
-        assert bias.dtype == torch.float32 and bias.device == dev and bias.stride(-1) == 1 and bias.shape in ((V,), (B, V))
-    strides = (0, 0)
+        assert bias.dtype is _float32 and bias.get_device() == dev and bias.stride(-1) == 1 and bias.shape in ((V,), (B, V))
+        bias_at, bias_stride = bias.data_ptr(), bias.stride(0) if bias.dim() == 2 else 0
     if allowed is not None:
-        assert allowed.dtype == torch.int32 and allowed.device == dev and allowed.stride(-1) == 1
+        assert allowed.dtype is _int32 and allowed.get_device() == dev and allowed.stride(-1) == 1
         assert allowed.shape[0] == B and allowed.shape[-1] >= (V + 31) // 32
         assert allowed.dim() == 2 or (allowed.dim() == 3 and allowed.shape[1] == R)
-        strides = (allowed.stride(0), allowed.stride(1) if allowed.dim() == 3 else 0)
-    nodes = 0
+        allowed_at, allowed_seq, allowed_row = allowed.data_ptr(), allowed.stride(0), allowed.stride(1) if allowed.dim() == 3 else 0
     if node_token is not None:
         assert node_token.dim() == 2 and node_parent is not None
         nodes = node_token.shape[1]
-    a = c2t_logit_rules(BF16 if logits.dtype == torch.bfloat16 else F32, B, R, V, logits.data_ptr(), out.data_ptr(), logits.stride(0),
-                        logits.stride(1), out.stride(0), out.stride(1), _ints(n_rows, B, dev), _dp(counts),
-                        counts.stride(0) if counts is not None else 0, _dp(repetition), _dp(frequency), _dp(presence), _dp(bias),
-                        bias.stride(0) if bias is not None and bias.dim() == 2 else 0, _dp(allowed), *strides, nodes,
-                        _ints(node_token, B * nodes, dev), _ints(node_parent, B * nodes, dev), _ints(row_node, B * R, dev))
-    with torch.cuda.device(dev):
-        _check(_calls().c2t_penalize_logits(C.byref(a), _stream(stream)), "c2t_penalize_logits")
+    rules = C.create_string_buffer(_RULES.size)
+    _RULES.pack_into(rules, 0, BF16 if dtype is torch.bfloat16 else F32, B, R, V, logits.data_ptr(), out.data_ptr(), ins[0], ins[1], outs[0],
+                     outs[1], _ints(n_rows, B, dev), counts_at, counts_stride, _floats(repetition, B, dev), _floats(frequency, B, dev),
+                     _floats(presence, B, dev), bias_at, bias_stride, allowed_at, allowed_seq, allowed_row, nodes,
+                     _ints(node_token, B * nodes, dev), _ints(node_parent, B * nodes, dev), _ints(row_node, B * R, dev))
+    rc = _device_call(dev, _calls().c2t_penalize_logits, C.cast(rules, C.POINTER(c2t_logit_rules)), _stream_on(dev, stream))
+    if rc:
+        _check(rc, "c2t_penalize_logits")
 
 
 def c2t_count_tokens(counts: torch.Tensor, tokens: torch.Tensor, n: torch.Tensor, index: Optional[torch.Tensor] = None,
                      plus_one: bool = False, delta: int = 1, stream=None) -> None:
     """counts: [B, V] int32; tokens: [B, N] int32; n: [B] int32; index: [B, width] int32.  With c2t_build_verify's tokens and
     c2t_accept's accept_len (plus_one: the root counts too) and path, the accepted tokens enter the history."""
-    dev = counts.device
-    assert counts.is_cuda and counts.dtype == torch.int32 and counts.dim() == 2 and counts.stride(1) == 1
+    dev = counts.get_device()
+    assert counts.is_cuda and counts.dtype is _int32 and counts.dim() == 2 and counts.stride(1) == 1
     B, V = counts.shape
     assert tokens.dim() == 2 and (index is None or index.dim() == 2)
-    width = tokens.shape[1] if index is None else index.shape[1]
-    with torch.cuda.device(dev):
-        _check(_calls().c2t_count_tokens(counts.data_ptr(), counts.stride(0), B, V, _ints(tokens, B * tokens.shape[1], dev),
-                                         tokens.shape[1], _ints(index, B * width, dev), width, _ints(n, B, dev), int(plus_one), width,
-                                         delta, _stream(stream)), "c2t_count_tokens")
+    N = tokens.shape[1]
+    width = N if index is None else index.shape[1]
+    rc = _device_call(dev, _calls().c2t_count_tokens, counts.data_ptr(), counts.stride(0), B, V, _ints(tokens, B * N, dev), N,
+                      _ints(index, B * width, dev), width, _ints(n, B, dev), int(plus_one), width, delta, _stream_on(dev, stream))
+    if rc:
+        _check(rc, "c2t_count_tokens")

@@ -130,3 +130,13 @@ def test_counts_that_are_refused(L):
 def test_config_still_refuses_float16_logits():
     s = c2t.Config(batch=1, vocab=100, dtype=c2t.F16, classifier=c2t.CLS_IDENTITY_JOINT)
     assert c2t.c2t_workspace_bytes(s) == 0
+
+
+def test_packed_structures_have_the_layout_of_c():
+    """What a call packs in one step is what the ctypes structures, field by field, say."""
+    from paper_2502_13652_b200 import kv_cache as K
+    for packed, struct in ((K._ATTENTION, c2t_attention), (K._RULES, c2t_logit_rules)):
+        assert packed.size <= C.sizeof(struct) < packed.size + 8
+        values = [float(i + 1) / 2 if t is C.c_float else i + 1 for i, (_, t) in enumerate(struct._fields_)]
+        got = struct.from_buffer_copy(packed.pack(*values) + bytes(8))
+        assert [getattr(got, name) for name, _ in struct._fields_] == values
