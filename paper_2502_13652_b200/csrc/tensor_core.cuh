@@ -49,6 +49,11 @@ __device__ __forceinline__ void copy_box(uint32_t to, const TensorMap *map, uint
                ::"r"(to), "l"(reinterpret_cast<uint64_t>(map)), "r"(shared_address(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
 
+__device__ __forceinline__ void copy_box(uint32_t to, const TensorMap *map, uint64_t *bar, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(to), "l"(reinterpret_cast<uint64_t>(map)), "r"(shared_address(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
 // ---------------------------------------------------------------- tensor memory
 
 __device__ __forceinline__ void tmem_alloc(uint32_t *address, int columns) {     // one whole warp

@@ -109,6 +109,7 @@ struct Params {
   int group, blocks_per_seq;                // query heads of a key head; blocks of max_queries * group rows
   uint32_t group_inverse;                   // 2^32 / group, rounded up (group > 1)
   int box_rows;                             // tokens of one copy: a page's, at most a tile's
+  int copy_queries;                         // 1: queries come by copies of kQueryRows rows, whole tokens; 0: thread by thread
   int split;                                // 1: tiles are dealt out evenly, blocks of rows may be cut; 0: whole blocks
   float *part_o;                            // [2 G][kBlockRows][D]: unfinished sums over the values, two per thread block
   float2 *part_ml;                          // [2 G][kBlockRows]: their maximum (scaled, base 2) and sum of weights
@@ -118,7 +119,8 @@ struct Params {
 // row -> (new token, query head of the group); rows * group < 2^32, which makes the inverse exact
 __device__ __forceinline__ int token_of(const Params &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_inverse); }
 
-struct Maps { TensorMap k, v; };
+struct Maps { TensorMap k, v, q; };
+constexpr int kQueryRows = 32;              // rows of queries that one copy brings
 
 struct Block {                              // with the tiles [k0, k1) of it that a thread block takes
   int b, head, row0, rows;                  // key head; first row; rows that are there (0: no block)
@@ -206,19 +208,21 @@ struct alignas(1024) Shared {
   unsigned char q[2][kRows * D * 2];        // 64 elements of all rows after the other 64; at a block's end its sums over the values
   union {
     unsigned char ring[Ring<D>::n][Ring<D>::bytes];
-    int before[C2T_MAX_BATCH + 1];          // while the work is dealt out: tiles of the pairs before
+    long long before[C2T_MAX_BATCH + 1];    // while the work is dealt out: of the pairs before, tiles and (upper half) how many have any
   };
   float2 ml[2][kRows];
   uint64_t full[Ring<D>::n], empty[Ring<D>::n];
-  uint64_t logits[2], weights[2], done, queries, meet, described[kBlocks], read[kBlocks];
+  uint64_t logits[2], weights[2], done, queries, queries_free, meet, described[kBlocks], read[kBlocks];
   Block block[kBlocks];
   uint32_t tmem;
   int gave_up;
   uint32_t odd[8];
-  int warp_sum[kThreads / 32], left, pair, head, k0;
+  long long warp_sum[kThreads / 32];
+  int most, left, pair, head, k0;
 };
 
 constexpr int kMaxPairs = C2T_MAX_BATCH;    // for an even deal
+constexpr int kWholeTiles = 8;              // of a block of rows that is not cut where every one finds a thread block
 
 template <int D>
 __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
@@ -262,6 +266,9 @@ __device__ __forceinline__ int last_box(int there, int box_rows) { return there 
 __device__ __forceinline__ int shift_of_last_box(int there, int box_rows) {
   return there >= kTile || there <= 0 ? 0 : last_box(there, box_rows) + box_rows - there;
 }
+
+// rows of one of the copies of a block's rows
+__device__ __forceinline__ int rows_of_copy(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : kRows; }
 
 // bits 0..31: columns c < n
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
@@ -553,34 +560,40 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     for (int s = 0; s < 2; ++s) { barrier_init(sh.logits + s, 1); barrier_init(sh.weights + s, kRows); }
     for (int i = 0; i < kBlocks; ++i) { barrier_init(sh.described + i, 1); barrier_init(sh.read + i, kReaders); }
     barrier_init(&sh.done, 1);
-    barrier_init(&sh.queries, kSoftmaxThreads);
+    barrier_init(&sh.queries, p.copy_queries ? 1 : kSoftmaxThreads);
+    barrier_init(&sh.queries_free, kSoftmaxThreads);
     barrier_init(&sh.meet, kSoftmaxThreads);
     barrier_init_fence();
     sh.gave_up = 0;
     sh.left = 0;
     tensor_map_prefetch(&maps.k);
     tensor_map_prefetch(&maps.v);
+    if (p.copy_queries) tensor_map_prefetch(&maps.q);
+    sh.most = 0;
   }
   chain_wait();
 
   // ---- the thread block's share of the tiles
+  __syncthreads();
   if (p.split) {
-    int carry = 0;
+    long long carry = 0;
 #pragma unroll 1
     for (int base = 0; base < n_pairs; base += kThreads) {
-      const int pair = base + tid, mine = pair < n_pairs ? block_of(p, pair).tiles : 0;
-      int x = mine;
+      const int pair = base + tid, tiles = pair < n_pairs ? block_of(p, pair).tiles : 0;
+      const long long mine = (tiles > 0 ? 1ll << 32 : 0) + tiles;
+      if (tiles > kWholeTiles) sh.most = tiles;                 // (any of those)
+      long long x = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(~0u, x, d);
+        const long long y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
       }
       if (lane == 31) sh.warp_sum[warp] = x;
       __syncthreads();
-      int earlier = 0, all = 0;
+      long long earlier = 0, all = 0;
 #pragma unroll
       for (int v = 0; v < kThreads / 32; ++v) {
-        const int s = sh.warp_sum[v];
+        const long long s = sh.warp_sum[v];
         earlier += v < warp ? s : 0;
         all += s;
       }
@@ -590,23 +603,31 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     }
     if (tid == 0) sh.before[n_pairs] = carry;
     __syncthreads();
-    const Deal deal(carry * p.c.kv_heads, G);
-    const int begin = deal.begin(blockIdx.x), left = deal.begin(blockIdx.x + 1) - begin;
+    // Few short blocks of rows go to a thread block each, uncut: adding up parts takes longer than the tiles do.
+    const int H = p.c.kv_heads, blocks = (int)(carry >> 32) * H;
+    const bool whole = blocks <= G && sh.most == 0;
+    const Deal deal((int)carry * H, G);
+    const int begin = whole ? (int)blockIdx.x : deal.begin(blockIdx.x), left = whole ? 0 : deal.begin(blockIdx.x + 1) - begin;
     if (tid == 0) {
       sh.left = left;
-      if (left == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      if (whole || left == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
     }
+    __syncthreads();
 #pragma unroll 1
-    for (int pair = tid; pair < n_pairs && left > 0; pair += kThreads) {
-      const int first = sh.before[pair] * p.c.kv_heads, mine = sh.before[pair + 1] - sh.before[pair];
-      if (begin < first || begin >= first + mine * p.c.kv_heads) continue;      // (one pair of one thread)
-      const int head = (begin - first) / mine, k0 = begin - first - head * mine;
+    for (int pair = tid; pair < n_pairs && (whole || left > 0); pair += kThreads) {
+      const int tiles = (int)sh.before[pair + 1] - (int)sh.before[pair], each = whole ? (tiles > 0) : tiles;      // of a head
+      const int first = (whole ? (int)(sh.before[pair] >> 32) : (int)sh.before[pair]) * H;
+      if (begin < first || begin >= first + each * H) continue;                 // (one pair of one thread, or none)
+      const int head = (begin - first) / each, k0 = begin - first - head * each;
       sh.pair = pair;
       sh.head = head;
       sh.k0 = k0;
-      // a block of rows that the thread block before this one began
-      const int c0 = k0 > 0 ? deal.owner(begin - k0) : -1;
-      p.cut[blockIdx.x] = k0 > 0 && c0 == (int)blockIdx.x - 1 ? make_int4(pair, head, c0, deal.owner(begin - k0 + mine - 1)) : make_int4(-1, 0, 0, 0);
+      if (whole) {
+        sh.left = tiles;
+      } else {                              // a block of rows that the thread block before this one began?
+        const int c0 = k0 > 0 ? deal.owner(begin - k0) : -1;
+        p.cut[blockIdx.x] = k0 > 0 && c0 == (int)blockIdx.x - 1 ? make_int4(pair, head, c0, deal.owner(begin - k0 + each - 1)) : make_int4(-1, 0, 0, 0);
+      }
     }
   }
   tmem_fence_before();
@@ -638,6 +659,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     if (lane == 0) {
       int left = sh.left, pair = p.split ? sh.pair : 0, head = p.split ? sh.head : blockIdx.x, k0 = p.split ? sh.k0 : 0, known = -1;
       Block w;
+      int copied = 0;                       // blocks whose queries were asked for
       for (int i = 0;; ++i) {
         bool more = false;
 #pragma unroll 1
@@ -660,7 +682,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         sh.block[i % kBlocks] = w;
         barrier_arrive(sh.described + i % kBlocks);
         if (!more) break;
+        if (p.copy_queries) {               // once the last block's sums are out of their memory
+          if (i > 0 && !wait(sh, &sh.queries_free, (i - 1) & 1)) break;
+          const bool two = w.rows > kRows;
+          const int boxes = (two ? 2 : 1) * kRows / kQueryRows, copy_rows = rows_of_copy(w.rows);
+          barrier_expect(&sh.queries, boxes * kQueryRows * D * 2);
+          ++copied;
+#pragma unroll 1
+          for (int x = 0; x < boxes; ++x) {
+            const int row = two ? x * kQueryRows : x * kQueryRows & (copy_rows - 1);
+#pragma unroll 1
+            for (int h = 0; h < D / 64; ++h)
+              copy_box(shared_address(sh.q[0]) + (x >> 2) * (kRows * D * 2) + h * (kRows * 128) + (x & 3) * (kQueryRows * 128), &maps.q, &sh.queries, h * 64,
+                       w.head * p.group, token_of(p, w.row0 + row), w.b);
+          }
+        }
       }
+      if (copied > 0 && *(volatile int *)&sh.gave_up)           // nothing may arrive in a block's memory that has ended
+        for (int tries = 0; tries < kTries && !barrier_try(&sh.queries, (copied - 1) & 1); ++tries) {}
     }
     __syncwarp();
   } else if (warp == 9) {
@@ -819,13 +858,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       const Block &w = sh.block[item % kBlocks];
       if (w.rows == 0) break;
       const bool two = w.rows > kRows;
-      const int copy_rows = w.rows <= 32 ? 32 : w.rows <= 64 ? 64 : kRows;      // rows of a copy
+      const int copy_rows = rows_of_copy(w.rows);
       const int n = w.k1 - w.k0, ahead = two ? 1 : 2;
-      ok = load_queries<T, D>(p, w, sh.q[0], copy_rows, [&] { return item == 0 || all_meet(); });       // (no sums of the last block in there any more)
-      if (!ok) break;
-      shared_writes_fence();
-      tmem_fence_before();
-      barrier_arrive(&sh.queries);
+      if (!p.copy_queries) {                // (once no sums of the last block are in their memory any more)
+        if (!(ok = load_queries<T, D>(p, w, sh.q[0], copy_rows, [&] { return item == 0 || all_meet(); }))) break;
+        shared_writes_fence();
+        tmem_fence_before();
+        barrier_arrive(&sh.queries);
+      }
 
       const int my_row = two ? s * kRows + row : row & (copy_rows - 1);         // in the block
       const int first_column = row & ~(copy_rows - 1);                          // of a copy's keys: as many as it has rows
@@ -978,6 +1018,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         once_more<T, D>(p, w, r, whole ? 0 : first_column, whole ? kTile : copy_rows, column0, columns, whole, __shfl_sync(~0u, m, from_lane),
                         p.part_o + (part * (D / 4) * kBlockRows + at) * 4);
       }
+      if (p.copy_queries) {
+        shared_writes_fence();
+        tmem_fence_before();
+        barrier_arrive(&sh.queries_free);
+      }
       block_read(item);
     }
   }
@@ -1103,6 +1148,20 @@ bool encode_pool(const c2t_cache &c, void *pool, int box_rows, TensorMap *map) {
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// (elements, heads, tokens, sequences); a box is 64 elements of kQueryRows rows: the heads of a key head, of as many tokens as that takes
+bool encode_queries(const c2t_cache &c, const c2t_attention &a, int group, TensorMap *map) {
+  const EncodeTiled encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t sizes[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.max_queries, (cuuint64_t)c.batch};
+  const int64_t steps[3] = {a.q_head_stride, a.q_token_stride, a.q_seq_stride};
+  cuuint64_t bytes[3];
+  for (int i = 0; i < 3; ++i) bytes[i] = sizes[i + 1] > 1 ? 2 * (cuuint64_t)steps[i] : 256;
+  const cuuint32_t box[4] = {64, (cuuint32_t)group, (cuuint32_t)(kQueryRows / group), 1}, ones[4] = {1, 1, 1, 1};
+  return encode(reinterpret_cast<CUtensorMap *>(map), c.dtype == C2T_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                const_cast<void *>(a.q_dev), sizes, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr int kMaxGrid = 256;               // workspaces are sized without asking the device: at most this many SMs are used
 
 struct Workspace { size_t o, ml, cut, bytes; };
@@ -1172,6 +1231,9 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
     cudaGetLastError();
     return C2T_ECUDA;
   }
+  // groups of heads that divide a copy's rows; no dimension without a stride, as broadcast queries have
+  const bool strides = (p.c.batch == 1 || p.a.q_seq_stride > 0) && (p.a.max_queries == 1 || p.a.q_token_stride > 0) && (p.a.q_heads == 1 || p.a.q_head_stride > 0);
+  p.copy_queries = strides && p.group <= kQueryRows && (p.group & (p.group - 1)) == 0 && encode_queries(p.c, p.a, p.group, &maps.q);
   if (sms > kMaxGrid) sms = kMaxGrid;
   const bool bf16 = p.c.dtype == C2T_BF16;
   auto launch = p.c.head_dim == 64 ? (bf16 ? launch_attention<__nv_bfloat16, 64> : launch_attention<__half, 64>)
