@@ -109,6 +109,7 @@ struct Params {
   int group, blocks_per_seq;                // query heads of a key head; blocks of max_queries * group rows
   uint32_t group_inverse;                   // 2^32 / group, rounded up (group > 1)
   int box_rows;                             // tokens of one copy: a page's, at most a tile's
+  int folded;                               // 1: small pages' keys and values come with both halves of a head in one box (one accumulator's blocks)
   int copy_queries;                         // 1: queries come by copies of kQueryRows rows, whole tokens; 0: thread by thread
   int split;                                // 1: tiles are dealt out evenly, blocks of rows may be cut; 0: whole blocks
   float *part_o;                            // [2 G][kBlockRows][D]: unfinished sums over the values, two per thread block
@@ -119,7 +120,7 @@ struct Params {
 // row -> (new token, query head of the group); rows * group < 2^32, which makes the inverse exact
 __device__ __forceinline__ int token_of(const Params &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_inverse); }
 
-struct Maps { TensorMap k, v, q; };
+struct Maps { TensorMap k, v, q, k_folded, v_folded; };
 constexpr int kQueryRows = 32;              // rows of queries that one copy brings
 
 struct Block {                              // with the tiles [k0, k1) of it that a thread block takes
@@ -222,7 +223,7 @@ struct alignas(1024) Shared {
 };
 
 constexpr int kMaxPairs = C2T_MAX_BATCH;    // for an even deal
-constexpr int kWholeTiles = 8;              // of a block of rows that is not cut where every one finds a thread block
+constexpr int kWholeTiles = 2;              // of a block of rows that is not cut where every one finds a thread block
 
 template <int D>
 __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
@@ -269,6 +270,9 @@ __device__ __forceinline__ int shift_of_last_box(int there, int box_rows) {
 
 // rows of one of the copies of a block's rows
 __device__ __forceinline__ int rows_of_copy(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : kRows; }
+
+// Do the columns of such a block's tiles take their keys from folded pages of 16, 8 of every page after the other 8?
+__device__ __forceinline__ bool is_woven(const Params &p, int rows) { return p.folded && rows <= kRows && p.box_rows == 16; }
 
 // bits 0..31: columns c < n
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
@@ -525,10 +529,15 @@ __device__ __noinline__ void once_more(const Params &p, const Block &w, int r, i
 #pragma unroll 1
   for (int t = w.k0; t < w.k1; ++t) {
     const int key = w.key0(t), last = last_box(w.keys - key, p.box_rows), over = shift_of_last_box(w.keys - key, p.box_rows);
+    const bool woven = is_woven(p, w.rows) && size < kTile;
 #pragma unroll 1
-    for (int shifted = 0; shifted < 2; ++shifted) {
-      const int lo = shifted ? max(first - over, last) : first, hi = shifted ? first + size - over : min(first + size, last);
-      if (!shifted || last < kTile) attend_row<T, D>(p.c, p.a, see, w.b, i, h, key + lo, min(key + hi, w.keys), m, l, o);
+    for (int c = first; c < first + size; c += woven ? 8 : size) {              // columns whose keys are side by side
+      const int slot = woven ? (c & 63) / 8 * 16 + (c >> 6) * 8 : c, n = woven ? 8 : size;
+#pragma unroll 1
+      for (int shifted = 0; shifted < 2; ++shifted) {
+        const int lo = shifted ? max(slot - over, last) : slot, hi = shifted ? slot + n - over : min(slot + n, last);
+        if (!shifted || last < kTile) attend_row<T, D>(p.c, p.a, see, w.b, i, h, key + lo, min(key + hi, w.keys), m, l, o);
+      }
     }
   }
   const float f = l == 0.f ? 0.f : finish ? 1.f / l : exp2f(m - part_m);
@@ -704,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     __syncwarp();
   } else if (warp == 9) {
     // ------------------------------------------------------------ copies
-    const int parts = kTile / p.box_rows, box_bytes = p.box_rows * 128, boxes = parts * (D / 64);
+    const int parts = kTile / p.box_rows, box_bytes = p.box_rows * 128;
     const int half = lane / parts, part = lane % parts, page_shift = __ffs(p.c.page_size) - 1;
     Cursor<kRing> to = {0, 0};
     int filled = 0;
@@ -715,6 +724,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       block_read(item);
       if (w.rows == 0) break;
       const int n = w.k1 - w.k0, ahead = w.rows > kRows ? 1 : 2, lead = min(n, ahead);
+      const bool folded = p.folded && w.rows <= kRows;
+      const int boxes = folded ? parts : parts * (D / 64);
       if (w.head == 0 && w.k0 == 0 && w.row0 == 0 && lane == 0 && w.keys < w.prefix + w.n) cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
       const int32_t *table = p.c.table_dev + (long long)w.b * p.c.max_pages;
       // the next copy of the order and the page that this lane copies for it (behind the pool: zeros)
@@ -737,9 +748,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           cache_fault(p.c, w.b, C2T_ST_BAD_PAGE);
         }
         __syncwarp();
-        if (lane < boxes)
-          copy_box(shared_address(sh.ring[to.at]) + half * (kTile * 128) + part * box_bytes, values ? &maps.v : &maps.k, sh.full + to.at, half * 64, w.head,
-                   (key & (p.c.page_size - 1)) - (key < w.keys ? max(key + p.box_rows - w.keys, 0) : 0), page, p.a.layer);
+        const int place = (key & (p.c.page_size - 1)) - (key < w.keys ? max(key + p.box_rows - w.keys, 0) : 0);
+        const uint32_t at = shared_address(sh.ring[to.at]);
+        if (lane < boxes && folded)
+          copy_box(at + part * (2 * box_bytes), values ? &maps.v_folded : &maps.k_folded, sh.full + to.at, 0, place, 0, w.head, page);
+        else if (lane < boxes)
+          copy_box(at + half * (kTile * 128) + part * box_bytes, values ? &maps.v : &maps.k, sh.full + to.at, half * 64, w.head, place, page, p.a.layer);
         to.step(1);
         ++filled;
         page = next; values = next_values; key = next_key;
@@ -756,33 +770,42 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
     // The whole warp goes along, so that what the instructions take lies in uniform registers; one lane issues them.
-    constexpr uint32_t kLogits = product_descriptor(kBf16, kTile, false), kMix = product_descriptor(kBf16, D, true);
-    const uint64_t q_tile = tile_descriptor(shared_address(sh.q[0]), 1024, 16), k_tile = tile_descriptor(shared_address(sh.ring[0]), 1024, 16),
-                   v_tile = tile_descriptor(shared_address(sh.ring[0]), 1024, kTile * 128);
+    constexpr uint32_t kLogits = product_descriptor(kBf16, kTile, false), kHalfLogits = product_descriptor(kBf16, kTile / 2, false), kMix = product_descriptor(kBf16, D, true);
+    const uint32_t ring = shared_address(sh.ring[0]);
+    const uint64_t q_tile = tile_descriptor(shared_address(sh.q[0]), 1024, 16);
     const bool leader = elect_one();
     Cursor<kRing> keys = {0, 0}, vals;
     uint32_t weights_parity = 0;            // of both
     bool ok = true;
     int item = 0;
     auto arrived = [&](uint64_t *bar, uint32_t parity) { return warp_wait(sh, bar, parity); };
+    // How a tile lies: 64 elements of its 128 keys after the other 64; or, folded, page by page both halves, 8 (16) keys each.  Of folded pages of 16 the
+    // first 8 keys of all pages are one product's columns and the others another's, and the columns come in this order.
+    struct Layout {
+      uint64_t k, v;
+      int k_half, products, v_step, v_jump; // to the other half; of 128 / products columns; from one step of 16 columns to the next, of four to four
+    } layout;
     auto logits = [&](int s, int half, int buffer) {
-      const uint64_t a = q_tile + half * (kRows * D * 2 / 16), b = k_tile + (uint32_t)buffer * (Ring<D>::bytes / 16);
+      const uint64_t a = q_tile + half * (kRows * D * 2 / 16);
       if (leader) {
+#pragma unroll 1
+        for (int x = 0; x < layout.products; ++x) {
+          const uint64_t b = layout.k + (uint32_t)(buffer * (Ring<D>::bytes / 16) + x * (1024 / 16));
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {                      // 64 elements, then the other 64; 16 of them a step
-          const int off = ((d >> 2) * (kTile * 128) + (d & 3) * 32) / 16;
-          product_shared(tmem + s * kTile, a + off, b + off, kLogits, d > 0);
+          for (int d = 0; d < D / 16; ++d)  // 64 elements, then the other 64; 16 of them a step
+            product_shared(tmem + s * kTile + x * 64, a + ((d >> 2) * (kRows * 128) + (d & 3) * 32) / 16, b + (d >> 2) * layout.k_half + (d & 3) * 2,
+                           layout.products == 1 ? kLogits : kHalfLogits, d > 0);
         }
         products_commit(sh.logits + s);
       }
       __syncwarp();
     };
     auto mix = [&](int s, int buffer, bool add) {
-      const uint64_t b = v_tile + (uint32_t)buffer * (Ring<D>::bytes / 16);
+      const uint64_t b = layout.v + (uint32_t)buffer * (Ring<D>::bytes / 16);
       if (leader) {
 #pragma unroll
         for (int d = 0; d < kTile / 16; ++d)
-          product_tensor(tmem + 256 + s * D, tmem + weights_at<D>(s) + d * 8, b + d * (2048 / 16), kMix, add || d > 0);
+          product_tensor(tmem + 256 + s * D, tmem + weights_at<D>(s) + d * 8, b + (d & 3) * layout.v_step + (d >> 2) * layout.v_jump, kMix, add || d > 0);
       }
       __syncwarp();
     };
@@ -799,6 +822,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       // (tile, half), else the tiles; two steps come first that have logits only.
       const bool two = rows > kRows;
       const int ahead = two ? 1 : 2, steps = two ? 2 * n : n;
+      const int box = p.folded && !two ? p.box_rows * 256 : 0;  // bytes of a folded page
+      layout.k = tile_descriptor(ring, box ? box : 1024, 16);
+      layout.v = tile_descriptor(ring, box ? box : 1024, box ? box / 2 : kTile * 128);
+      layout.k_half = (box ? box / 2 : kTile * 128) / 16;
+      layout.products = box == 4096 ? 2 : 1;
+      layout.v_step = (box ? 2 * box : 2048) / 16;
+      layout.v_jump = (box == 4096 ? 1024 : box ? 8 * box : 8192) / 16;
       vals = keys;
       vals.step(min(n, ahead));
       if (!(ok = arrived(&sh.queries, item & 1))) break;
@@ -872,6 +902,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       const bool live = my_row < w.rows;
       const bool warp_live = (my_row & ~31) < w.rows;
       const int node = token_of(p, w.row0 + (live ? my_row : w.rows - 1));
+      const bool woven = is_woven(p, w.rows);
       float m = -INFINITY, l = 0.f;
       {
         const Sight see = sight_of(p, w);
@@ -886,11 +917,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 #pragma unroll 1
             for (int i = copy_rows / 32; i > 0; --i) {
               on[3] = on[2]; on[2] = on[1]; on[1] = on[0];
-              const int c = first_column + 32 * (i - 1);
-              uint32_t word = 0;
+              // (folded pages of 16: a word's columns are 8 keys of four pages, from two words of keys)
+              const int at = first_column / 32 + i - 1;
+              uint32_t word = 0, other = 0;
 #pragma unroll 1
-              for (int shift = 0; shift <= over; shift += max(over, 1))         // the columns before the last box, then the box
-                word |= sight_bits(see, node, own, key + c - shift) & (shift ? ~low_bits(last + over - c) : low_bits(over ? last - c : 32));
+              for (int x = 0; x < (woven ? 2 : 1); ++x) {
+                const int c = 32 * (woven ? 2 * (at & 1) + x : at);
+                other = word;
+                word = 0;
+#pragma unroll 1
+                for (int shift = 0; shift <= over; shift += max(over, 1))       // the keys before the last box, then the box
+                  word |= sight_bits(see, node, own, key + c - shift) & (shift ? ~low_bits(last + over - c) : low_bits(over ? last - c : 32));
+              }
+              if (woven) word = __byte_perm(other, word, at >> 1 ? 0x7531 : 0x6420);
               on[0] = word;
             }
           }
@@ -1148,6 +1187,19 @@ bool encode_pool(const c2t_cache &c, void *pool, int box_rows, TensorMap *map) {
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// (64 elements, places of a page, halves of a head, heads, pages) of one layer; a box is a whole page's tokens of one head
+bool encode_folded(const c2t_cache &c, void *pool, int layer, TensorMap *map) {
+  const EncodeTiled encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t sizes[5] = {64, (cuuint64_t)c.page_size, 2, (cuuint64_t)c.kv_heads, (cuuint64_t)c.n_pages};
+  const cuuint64_t bytes[4] = {2 * (cuuint64_t)c.token_stride, 128, c.kv_heads > 1 ? 2 * (cuuint64_t)c.head_stride : 256,
+                               c.n_pages > 1 ? 2 * (cuuint64_t)c.page_stride : 256};
+  const cuuint32_t box[5] = {64, (cuuint32_t)c.page_size, 2, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+  return encode(reinterpret_cast<CUtensorMap *>(map), c.dtype == C2T_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+                static_cast<uint16_t *>(pool) + layer * c.layer_stride, sizes, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // (elements, heads, tokens, sequences); a box is 64 elements of kQueryRows rows: the heads of a key head, of as many tokens as that takes
 bool encode_queries(const c2t_cache &c, const c2t_attention &a, int group, TensorMap *map) {
   const EncodeTiled encode = encoder();
@@ -1234,6 +1286,10 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   // groups of heads that divide a copy's rows; no dimension without a stride, as broadcast queries have
   const bool strides = (p.c.batch == 1 || p.a.q_seq_stride > 0) && (p.a.max_queries == 1 || p.a.q_token_stride > 0) && (p.a.q_heads == 1 || p.a.q_head_stride > 0);
   p.copy_queries = strides && p.group <= kQueryRows && (p.group & (p.group - 1)) == 0 && encode_queries(p.c, p.a, p.group, &maps.q);
+  // Copies of 2 KB are dealt with at 140 cycles each, which is less than the memory gives; with both halves of a head in one, pages of 16 tokens cost
+  // (two products for the logits of half the columns each, which do not matter where the copies do) ...
+  p.folded = p.c.head_dim == 128 && p.c.page_size <= 16 && encode_folded(p.c, p.c.k_dev, p.a.layer, &maps.k_folded) &&
+             encode_folded(p.c, p.c.v_dev, p.a.layer, &maps.v_folded);
   if (sms > kMaxGrid) sms = kMaxGrid;
   const bool bf16 = p.c.dtype == C2T_BF16;
   auto launch = p.c.head_dim == 64 ? (bf16 ? launch_attention<__nv_bfloat16, 64> : launch_attention<__half, 64>)
