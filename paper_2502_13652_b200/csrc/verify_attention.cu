@@ -1084,69 +1084,117 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 
 // ---------------------------------------------------------------- parts of rows that several thread blocks read the keys of
 
-constexpr int kJoinThreads = 128;           // a quarter of the columns a warp
+// The parts of a cut block of rows lie with thread blocks c0 .. c1: the first's second place, then the others' first.  Of a part, 16 bytes of all rows lie
+// side by side.  Rows that lay in the accumulators in copies have a part for each.
+struct Parts {
+  const float *o;
+  const float2 *ml;
+  int4 cut;
+  int shift, copy_rows, n;                  // copies = 1 << shift; parts of a row
+  __device__ __forceinline__ Parts(const Params &p, const int4 &cut_, const Block &w) : o(p.part_o), ml(p.part_ml), cut(cut_) {
+    shift = w.rows > kRows ? 0 : w.rows <= 32 ? 2 : w.rows <= 64 ? 1 : 0;
+    copy_rows = kRows >> shift;
+    n = (cut.w - cut.z + 1) << shift;
+  }
+  __device__ __forceinline__ long long place(int i, int r) const {              // of row r's i-th part among all parts' rows
+    const int c = cut.z + (i >> shift);
+    return (2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows + r + (i & ((1 << shift) - 1)) * copy_rows;
+  }
+  template <int D>
+  __device__ __forceinline__ const float4 *sums(long long place) const {        // its first 4 columns; the next lie kBlockRows further
+    return reinterpret_cast<const float4 *>(o) + place / kBlockRows * (D / 4 * kBlockRows) + place % kBlockRows;
+  }
+};
 
-// Grid (G, parts of a block's rows).  The parts of a cut block of rows lie with thread blocks c0 .. c1: the first's second place, then the others' first.
-// Of a part, 16 bytes of all rows lie side by side.  Rows that lay in the accumulators in copies have a part for each.
-// kJoinRows lanes have a row each, and the 32 / kJoinRows lanes of a row every so many-th of its parts: with few rows the parts, one after the other, are
-// what the launch would wait for.
-template <typename T, int D, int kJoinRows>
+__device__ __forceinline__ float part_factor(const float2 &ml, float m) { return ml.x == -INFINITY ? 0.f : exp2f(ml.x - m); }
+__device__ __forceinline__ float part_sum(const float2 &ml, float f) { return ml.x == -INFINITY ? ml.y : ml.y * f; }   // (one that sees nothing: 0, or NaN)
+
+template <typename T>
+__device__ __forceinline__ T *joined_row(const Params &p, const Block &w, int head, int r, float m, float l, bool tell) {
+  const int at = w.row0 + r, node = token_of(p, at), h = head * p.group + at - node * p.group;
+  if (tell && p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  return static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + h * p.a.out_head_stride;
+}
+
+// Grid (G, 32 rows each): a row a lane, D / 8 columns a warp.
+constexpr int kJoinThreads = 256;
+template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(const __grid_constant__ Params p) {
   chain_enter();
   const int4 cut = p.cut[blockIdx.x];
   if (cut.x < 0) return;
   const Block w = block_of(p, cut.x);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * kJoinRows + lane % kJoinRows;
-  const bool there = r < w.rows;
-  const int shift = w.rows > kRows ? 0 : w.rows <= 32 ? 2 : w.rows <= 64 ? 1 : 0, copy_rows = kRows >> shift;
-  const int n = there ? (cut.w - cut.z + 1) << shift : 0;
-  constexpr int kColumns = D / 4;           // of a warp
-  // the i-th part: its thread block's place, and the row's among its rows
-  auto place = [&](int i) {
-    const int c = cut.z + (i >> shift);
-    return (2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows * (D / 4) + (r + (i & ((1 << shift) - 1)) * copy_rows);
-  };
-  auto ml_of = [&](int i) {
-    const int c = cut.z + (i >> shift);
-    return p.part_ml[(2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows + r + (i & ((1 << shift) - 1)) * copy_rows];
-  };
+  const int warp = threadIdx.x >> 5, r = blockIdx.y * 32 + (threadIdx.x & 31);
+  if (r >= w.rows) return;
+  const Parts parts(p, cut, w);
+  constexpr int kVectors = D / 32;          // of 4 columns
   float m = -INFINITY, l = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < parts.n; ++i) m = fmaxf(m, parts.ml[parts.place(i, r)].x);
+  float4 o[kVectors];
+#pragma unroll
+  for (int j = 0; j < kVectors; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int i = lane / kJoinRows; i < n; i += 32 / kJoinRows) m = fmaxf(m, ml_of(i).x);
+  for (int i = 0; i < parts.n; ++i) {
+    const long long place = parts.place(i, r);
+    const float2 ml = parts.ml[place];
+    const float4 *from = parts.sums<D>(place) + warp * kVectors * kBlockRows;
+    const float f = part_factor(ml, m);
+    l += part_sum(ml, f);
 #pragma unroll
-  for (int d = kJoinRows; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-  float o[kColumns];
-#pragma unroll
-  for (int j = 0; j < kColumns; ++j) o[j] = 0.f;
-#pragma unroll 2
-  for (int i = lane / kJoinRows; i < n; i += 32 / kJoinRows) {
-    const float2 ml = ml_of(i);
-    const float4 *from = reinterpret_cast<const float4 *>(p.part_o) + place(i) + warp * (kColumns / 4) * kBlockRows;
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
-    l += ml.x == -INFINITY ? ml.y : ml.y * f;                   // (a part that sees nothing: 0, or NaN)
-#pragma unroll
-    for (int j = 0; j < kColumns; j += 4) {
-      const float4 x = from[(j / 4) * kBlockRows];
-      o[j] = fmaf(x.x, f, o[j]); o[j + 1] = fmaf(x.y, f, o[j + 1]); o[j + 2] = fmaf(x.z, f, o[j + 2]); o[j + 3] = fmaf(x.w, f, o[j + 3]);
+    for (int j = 0; j < kVectors; ++j) {
+      const float4 x = from[j * kBlockRows];
+      o[j].x = fmaf(x.x, f, o[j].x); o[j].y = fmaf(x.y, f, o[j].y); o[j].z = fmaf(x.z, f, o[j].z); o[j].w = fmaf(x.w, f, o[j].w);
     }
   }
-#pragma unroll
-  for (int d = kJoinRows; d < 32; d <<= 1) {
-    l += __shfl_xor_sync(~0u, l, d);
-#pragma unroll
-    for (int j = 0; j < kColumns; ++j) o[j] += __shfl_xor_sync(~0u, o[j], d);
-  }
-  if (!there) return;
-  const int at = w.row0 + r, node = token_of(p, at), head = cut.y * p.group + at - node * p.group;
   const float share = l == 0.f ? 0.f : 1.f / l;
-  T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + head * p.a.out_head_stride + warp * kColumns;
-  if (lane < kJoinRows)
+  T *out = joined_row<T>(p, w, cut.y, r, m, l, warp == 0) + warp * (D / 8);
 #pragma unroll
-    for (int j = 0; j < kColumns; j += 8)
-      *reinterpret_cast<uint4 *>(out + j) = make_uint4(pack<T>(o[j] * share, o[j + 1] * share), pack<T>(o[j + 2] * share, o[j + 3] * share),
-                                                       pack<T>(o[j + 4] * share, o[j + 5] * share), pack<T>(o[j + 6] * share, o[j + 7] * share));
-  if (p.a.lse_dev && warp == 0 && lane < kJoinRows)
-    p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  for (int j = 0; j < kVectors; ++j)
+    *reinterpret_cast<uint2 *>(out + 4 * j) = make_uint2(pack<T>(o[j].x * share, o[j].y * share), pack<T>(o[j].z * share, o[j].w * share));
+}
+
+// Grid (G, rows): few rows have many parts each (copies too), which one after the other are what the launch would wait for.  A row a block, every so
+// many-th part a group of D / 4 lanes, 4 columns a lane.
+template <typename T, int D>
+__global__ void __launch_bounds__(kJoinThreads) join_few_kernel(const __grid_constant__ Params p) {
+  chain_enter();
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  __shared__ float4 sums[kGroups][kLanes];
+  __shared__ float total[kGroups];
+  const int4 cut = p.cut[blockIdx.x];
+  if (cut.x < 0) return;
+  const Block w = block_of(p, cut.x);
+  const int r = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x / kLanes, column = threadIdx.x % kLanes;
+  if (r >= w.rows) return;
+  const Parts parts(p, cut, w);
+  float m = -INFINITY, l = 0.f;
+  for (int i = lane; i < parts.n; i += 32) m = fmaxf(m, parts.ml[parts.place(i, r)].x);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = group; i < parts.n; i += kGroups) {
+    const long long place = parts.place(i, r);
+    const float2 ml = parts.ml[place];
+    const float4 x = parts.sums<D>(place)[column * kBlockRows];
+    const float f = part_factor(ml, m);
+    l += part_sum(ml, f);
+    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+  }
+  sums[group][column] = o;
+  if (column == 0) total[group] = l;
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) {
+    const float4 x = sums[g][column];
+    o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    l = g == 1 ? total[0] + total[1] : l + total[g];
+  }
+  const float share = l == 0.f ? 0.f : 1.f / l;
+  T *out = joined_row<T>(p, w, cut.y, r, m, l, column == 0) + 4 * column;
+  *reinterpret_cast<uint2 *>(out) = make_uint2(pack<T>(o.x * share, o.y * share), pack<T>(o.z * share, o.w * share));
 }
 
 int check_attention(const c2t_cache *c, const c2t_attention *a) {
@@ -1248,8 +1296,8 @@ cudaError_t launch_attention(const Params &p, const Maps &maps, int sms, cudaStr
   if (e == cudaSuccess && p.split) {
     const long long rows = (long long)p.a.max_queries * p.group;
     const int most = (int)(rows < kBlockRows ? rows : kBlockRows);
-    if (most <= 32) e = launch_chained(join_parts_kernel<T, D, 8>, dim3(sms, (most + 7) / 8), dim3(kJoinThreads), 0, s, p);
-    else e = launch_chained(join_parts_kernel<T, D, 32>, dim3(sms, (most + 31) / 32), dim3(kJoinThreads), 0, s, p);
+    if (most <= 32) e = launch_chained(join_few_kernel<T, D>, dim3(sms, most), dim3(kJoinThreads), 0, s, p);
+    else e = launch_chained(join_parts_kernel<T, D>, dim3(sms, (most + 31) / 32), dim3(kJoinThreads), 0, s, p);
   }
   return e;
 }
