@@ -24,9 +24,12 @@ int check_cache(const c2t_cache *c) {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;
+// The planning kernels are one block each and wait for memory and for one another's warps, round by round.  A first round of 2048 counts, then of 8192, by
+// 512 threads: a fork of 8 slots and its three other launches take 19.4 us, with 16384 counts a round by 1024 threads 29.3 (64 slots' room given and taken back:
+// 5.9, 9.8); where the 256 free pages are the last of 131072, 36.1 and 33.2, with 256 threads 49.8.
+constexpr int kPlanThreads = 512;
 constexpr int kPlanWarps = kPlanThreads / 32;
-constexpr int kScan = 16;                   // counts per lane and round of the search for free pages
+constexpr int kFirstScan = 4, kScan = 16;   // counts per lane and round of the search for free pages
 constexpr int kCopyThreads = 256;
 
 // position -> element offset without layer and head, -1 where the slot has no page for it
@@ -76,50 +79,60 @@ __device__ void sum_needs(PlanShared &sh, int B) {
   __syncthreads();
 }
 
+// One round of take_pages: the counts [base, base + kPlanThreads * n), each warp over a part of its own in ascending order.
+template <int n, typename First>
+__device__ int take_round(const c2t_cache &c, PlanShared &sh, long long base, int total, int taken, First first) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long at = base + warp * (32 * n) + lane;
+  int ref[n];
+#pragma unroll
+  for (int i = 0; i < n; ++i) ref[i] = at + 32 * i < c.n_pages ? c.refs_dev[at + 32 * i] : 1;
+  unsigned free_mask[n];
+  int mine = 0;
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    free_mask[i] = __ballot_sync(~0u, ref[i] == 0);
+    mine += __popc(free_mask[i]);
+  }
+  if (lane == 0) sh.warp_sum[warp] = mine;
+  __syncthreads();
+  int rank = taken, all = 0;
+  for (int w = 0; w < kPlanWarps; ++w) {
+    const int s = sh.warp_sum[w];
+    rank += w < warp ? s : 0;
+    all += s;
+  }
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const int r = rank + __popc(free_mask[i] & ((1u << lane) - 1));
+    rank += __popc(free_mask[i]);
+    if (ref[i] != 0 || r >= total) continue;
+    int lo = 0, hi = c.batch;                          // the last slot whose offset is <= r: later ones with the same offset need nothing
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sh.offset[mid] <= r) lo = mid; else hi = mid;
+    }
+    c.refs_dev[at + 32 * i] = 1;
+    c.table_dev[(long long)lo * c.max_pages + first(lo) + r - sh.offset[lo]] = (int)(at + 32 * i);
+  }
+  __syncthreads();
+  return all;
+}
+
 // Gives free pages, in ascending order, to the needs in sh.offset (summed up): the r-th page to entry r - offset[b] of the slot b with
 // offset[b] <= r < offset[b + 1], behind the first[b] pages that it has.  Returns how many there were, at most the total.  One read of the
-// counts, in rounds of kPlanThreads * kScan, each warp over a part of its own in ascending order, until the needs are met.
+// counts, in rounds, until the needs are met: a short one first, since the free pages are often the first ones, then longer ones, which a
+// full pool asks for.
 template <typename First>
 __device__ int take_pages(const c2t_cache &c, PlanShared &sh, First first) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int total = sh.offset[c.batch];
   int taken = 0;
-  for (long long base = 0; base < c.n_pages && taken < total; base += kPlanThreads * kScan) {
-    const long long at = base + warp * (32 * kScan) + lane;
-    int ref[kScan];
-#pragma unroll
-    for (int i = 0; i < kScan; ++i) ref[i] = at + 32 * i < c.n_pages ? c.refs_dev[at + 32 * i] : 1;
-    unsigned free_mask[kScan];
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kScan; ++i) {
-      free_mask[i] = __ballot_sync(~0u, ref[i] == 0);
-      mine += __popc(free_mask[i]);
-    }
-    if (lane == 0) sh.warp_sum[warp] = mine;
-    __syncthreads();
-    int rank = taken, all = 0;
-    for (int w = 0; w < kPlanWarps; ++w) {
-      const int s = sh.warp_sum[w];
-      rank += w < warp ? s : 0;
-      all += s;
-    }
-#pragma unroll
-    for (int i = 0; i < kScan; ++i) {
-      const int r = rank + __popc(free_mask[i] & ((1u << lane) - 1));
-      rank += __popc(free_mask[i]);
-      if (ref[i] != 0 || r >= total) continue;
-      int lo = 0, hi = c.batch;                        // the last slot whose offset is <= r: later ones with the same offset need nothing
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (sh.offset[mid] <= r) lo = mid; else hi = mid;
-      }
-      c.refs_dev[at + 32 * i] = 1;
-      c.table_dev[(long long)lo * c.max_pages + first(lo) + r - sh.offset[lo]] = (int)(at + 32 * i);
-    }
-    taken += all;
-    __syncthreads();
+  long long base = 0;
+  if (total > 0) {
+    taken = take_round<kFirstScan>(c, sh, base, total, taken, first);
+    base += kPlanThreads * kFirstScan;
   }
+  for (; base < c.n_pages && taken < total; base += kPlanThreads * kScan) taken += take_round<kScan>(c, sh, base, total, taken, first);
   return taken < total ? taken : total;
 }
 
@@ -401,7 +414,7 @@ int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, con
   if (new_len_dev == prefix_len_dev || new_len_dev == accept_len_dev) return C2T_EINVAL;       // (other blocks still read those)
   if (path_width > kPathMax) return C2T_ERANGE;
   const long long threads = 2ll * cache->layers * cache->kv_heads * (cache->head_dim / 8);
-  if (threads > 0x7FFFFFFF) return C2T_ERANGE;
+  if (threads > 0x40000000) return C2T_ERANGE;
   return launched(launch_chained(compact_kernel, dim3(parts_for(threads, 4096), cache->batch), dim3(kCopyThreads), 0, (cudaStream_t)stream, *cache,
                                  prefix_len_dev, accept_len_dev, path_dev, path_width, new_len_dev, log2_of(cache->page_size)));
 }
