@@ -277,7 +277,8 @@ int c2t_penalize_logits(const c2t_logit_rules *rules, void *stream) {
   if (groups > 65535 || tiles > 65535) return C2T_ERANGE;
   const size_t smem = a.node_token_dev ? 2 * sizeof(int) * (size_t)a.nodes : 0;
   void (*kernel)(c2t_logit_rules, int) = a.dtype == C2T_BF16 ? penalize_kernel<__nv_bfloat16> : penalize_kernel<float>;
-  if (smem > 32768 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(int) * C2T_MAX_TREE) != cudaSuccess)
+  if (smem + sizeof(RuleShared) > 48 * 1024 &&                  // what a block has of both kinds without being asked for
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(int) * C2T_MAX_TREE) != cudaSuccess)
     return launched(cudaErrorUnknown);
   return launched(launch_chained(kernel, dim3(a.batch, groups, tiles), dim3(kRuleThreads), smem, (cudaStream_t)stream, a, rows_per_block));
 }

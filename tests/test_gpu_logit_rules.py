@@ -121,6 +121,11 @@ def test_many_nodes():
     check(x, a)
 
 
+def test_node_arrays_that_fit_alone_but_not_beside_a_blocks_own():
+    x, a = inputs(2, 5, 400, 2900, torch.float32, seed=12, draft=True)
+    check(x, a)
+
+
 def test_counts():
     B, V, N = 3, 50, 9
     tokens = torch.randint(0, V, (B, N), dtype=torch.int32)
