@@ -571,10 +571,12 @@ int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, con
  * A node's own position is position_ids[b, i] (c2t_build_verify's; NULL: prefix_len + i; a value below prefix_len[b] counts as
  * prefix_len[b]).  A row that sees nothing gets zeros and lse = -inf.  Keys and values that no mask lets a row see do not reach it,
  * whatever they hold (NaN and infinities included).
- * Query head h reads key head h / (q_heads / kv_heads).  Rows i >= n_queries[b] are neither read nor written.
+ * Query head h reads key head h / (q_heads / kv_heads).  Rows i >= n_queries[b] of out and lse are not written; what they hold in q does not
+ * matter.  out must not overlap q.  Strides of q may be 0, those of out that are stepped over may not.
  * n_queries is cut to max_queries; positions without a held page are not seen (C2T_ST_BAD_PAGE).  A page number out of range among the
  * held ones sets that bit too and leaves the slot's rows unspecified, but nothing out of bounds is touched.
- * Products are of 16 bits with 32-bit sums; the weights are rounded to the cache's type for the second product.
+ * A prefix_len below 0 counts as 0.
+ * Products are of 16 bits with 32-bit sums; the weights are rounded to the cache's type for the second product.  Two launches at most.
  */
 typedef struct {
   int32_t layer;
@@ -591,7 +593,7 @@ typedef struct {
   int32_t mask_words;
   const int32_t *position_ids_dev;   /* [B, Nq] or NULL                                                 */
   int32_t window, sinks;        /* 0 = no window; sinks >= 0                                            */
-  float scale;
+  float scale;                  /* > 0                                                                  */
 } c2t_attention;
 
 /* Workspace of c2t_verify_attention for such a call (0 on invalid sizes): the parts of rows whose keys are read by several thread

@@ -254,6 +254,7 @@ int c2t_penalize_logits(const c2t_logit_rules *rules, void *stream) {
   if (a.dtype != C2T_F32 && a.dtype != C2T_BF16) return C2T_EINVAL;
   if (a.batch < 1 || a.rows < 1 || a.vocab < 1) return C2T_EINVAL;
   if (a.in_seq_stride < 0 || a.out_seq_stride < 0 || a.in_row_stride < a.vocab || a.out_row_stride < a.vocab) return C2T_EINVAL;
+  if (a.batch > 1 && a.out_seq_stride < a.vocab) return C2T_EINVAL;             // (rows of two sequences in one place)
   if (a.counts_dev && a.counts_stride < a.vocab) return C2T_EINVAL;
   if (a.bias_dev && a.bias_stride != 0 && a.bias_stride < a.vocab) return C2T_EINVAL;
   if (a.allowed_dev && (a.allowed_seq_stride < 0 || a.allowed_row_stride < 0)) return C2T_EINVAL;
@@ -289,7 +290,7 @@ int c2t_count_tokens(int32_t *counts_dev, int64_t counts_stride, int32_t batch, 
   if (!counts_dev || !tokens_dev || !n_dev || batch < 1 || vocab < 1 || token_width < 1 || width < 1 || counts_stride < vocab) return C2T_EINVAL;
   if (plus_one != 0 && plus_one != 1) return C2T_EINVAL;
   if (width > (index_dev ? index_stride : token_width)) return C2T_EINVAL;
-  if (batch > C2T_MAX_BATCH) return C2T_ERANGE;
+  if (batch > C2T_MAX_BATCH || width > (1 << 30)) return C2T_ERANGE;
   return launched(launch_chained(count_tokens_kernel, dim3((width + kRuleThreads - 1) / kRuleThreads, batch), dim3(kRuleThreads), 0,
                                  (cudaStream_t)stream, counts_dev, counts_stride, vocab, tokens_dev, token_width, index_dev, index_stride, n_dev,
                                  plus_one, width, delta));

@@ -82,21 +82,9 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *r) {
                ::C2T_W4(r, 0), C2T_W4(r, 4), C2T_W4(r, 8), C2T_W4(r, 12), C2T_W4(r, 16), C2T_W4(r, 20), C2T_W4(r, 24), C2T_W4(r, 28), "r"(at) : "memory");
 }
 // 16 columns
-__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t *r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-               : C2T_R4(r, 0), C2T_R4(r, 4), C2T_R4(r, 8), C2T_R4(r, 12) : "r"(at) : "memory");
-}
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t *r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                ::C2T_W4(r, 0), C2T_W4(r, 4), C2T_W4(r, 8), C2T_W4(r, 12), "r"(at) : "memory");
-}
-template <int n>
-__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t *r) {
-  static_assert(n == 16 || n % 32 == 0, "columns of a load");
-  if (n == 16) tmem_load16(at, r);
-  else
-#pragma unroll
-    for (int i = 0; i < n; i += 32) tmem_load32(at + i, r + i);
 }
 #undef C2T_R4
 #undef C2T_W4

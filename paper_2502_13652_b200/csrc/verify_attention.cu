@@ -14,6 +14,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+constexpr int kMaxTokens = 0x40000000;      // of a slot; with the queries' number 32 bits hold every position
+
 // What the rows of a sequence see.
 struct Sight {
   int prefix, n, keys;                      // cached tokens, new tokens, positions with a held page
@@ -39,7 +41,7 @@ struct Sight {
 
 __device__ __forceinline__ Sight sight_of(const c2t_cache &c, const c2t_attention &a, int b) {
   Sight s;
-  s.prefix = max(a.prefix_len_dev[b], 0);
+  s.prefix = min(max(a.prefix_len_dev[b], 0), kMaxTokens);      // (no page holds a position behind that)
   s.n = min(max(a.n_queries_dev[b], 0), a.max_queries);
   const long long held = (long long)held_pages(c, b) * c.page_size, want = (long long)s.prefix + s.n;
   s.keys = (int)min(held, want);
@@ -195,7 +197,7 @@ constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x D; P in the place of S, with heads of 64 in columns of its own
 template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 14.f : 40.f;
 constexpr int kProducts = 1;                // of 8 powers of two that are not taken by the special-function unit: 2 kProducts / 2
-constexpr int kTries = 1 << 22;             // of a wait, after which the block gives up
+constexpr int kTries = 1 << 20;             // of a wait, 3900 cycles each: after two seconds the block gives up
 
 template <int D> __device__ __forceinline__ constexpr int weights_at(int s) { return D == 64 ? 384 + s * 64 : s * kTile; }
 
@@ -562,8 +564,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_pairs = p.c.batch * p.blocks_per_seq, G = gridDim.x;
 
-  chain_release();
-  if (warp == 8) tmem_alloc(&sh.tmem, kMathColumns);
+  if (warp == 8) {
+    tmem_alloc(&sh.tmem, kMathColumns);
+    chain_release();                        // (after it: a successor's blocks could take the tensor memory and wait for this one)
+  }
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { barrier_init(sh.full + i, 1); barrier_init(sh.empty + i, 1); }
     for (int s = 0; s < 2; ++s) { barrier_init(sh.logits + s, 1); barrier_init(sh.weights + s, kRows); }
@@ -639,6 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       }
     }
   }
+  shared_writes_fence();                    // (the ring's copies come where the sums were)
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -1211,6 +1216,10 @@ int check_attention(const c2t_cache *c, const c2t_attention *a) {
   if (!vector_aligned(a->q_dev) || !vector_aligned(a->out_dev)) return C2T_EALIGN;
   for (int64_t s : strides)
     if (!vector_stride(s)) return C2T_EALIGN;
+  // (two rows in one place)
+  if ((c->batch > 1 && a->out_seq_stride < c->head_dim) || (a->max_queries > 1 && a->out_token_stride < c->head_dim) ||
+      (a->q_heads > 1 && a->out_head_stride < c->head_dim))
+    return C2T_EINVAL;
   return C2T_OK;
 }
 

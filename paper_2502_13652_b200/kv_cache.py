@@ -101,7 +101,7 @@ class KVCache:
     k, v: [layers, n_pages, page_size, kv_heads, head_dim], bfloat16 or float16, equal strides, last dimension contiguous (any
     order of the others: `permute` a pool that is laid out head by head).  table: [batch, max_pages] int32, held: [batch] int32, refs:
     [n_pages] int32; `new_state` makes them for an empty cache.  q_heads, max_queries: the largest attention call that will
-    be made; without them the cache has no workspace and its other calls work.
+    be made; without them the cache has no workspace and its other calls work.  One thread at a time makes calls, as on a context.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, held: torch.Tensor, refs: torch.Tensor,

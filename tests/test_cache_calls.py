@@ -140,3 +140,14 @@ def test_packed_structures_have_the_layout_of_c():
         values = [float(i + 1) / 2 if t is C.c_float else i + 1 for i, (_, t) in enumerate(struct._fields_)]
         got = struct.from_buffer_copy(packed.pack(*values) + bytes(8))
         assert [getattr(got, name) for name, _ in struct._fields_] == values
+
+
+@pytest.mark.parametrize("what", ["out_seq_stride", "out_token_stride", "out_head_stride"])
+def test_rows_in_one_place_are_refused(L, what):
+    assert L.c2t_verify_attention(C.byref(cache()), C.byref(attention(**{what: 0})), A, 1 << 40, None) == c2t.EINVAL
+    assert L.c2t_penalize_logits(C.byref(rules(in_seq_stride=0, out_seq_stride=0)), None) == c2t.EINVAL
+
+
+def test_counts_of_more_entries_than_32_bits_reach(L):
+    n = (1 << 30) + 1
+    assert L.c2t_count_tokens(A, 1000, 2, 1000, A, n, None, 0, A, 0, n, 1, None) == c2t.ERANGE

@@ -320,3 +320,61 @@ def test_keys_behind_four_gigabytes():
     c.call()
     torch.cuda.synchronize()
     c.compare()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,n,H,D", [(1, [1, 0, 1], 4, 128), (60, [60, 17, 1], 4, 64), (60, [3, 60, 0], 8, 128), (150, [150, 70, 9], 4, 128), (40, [40, 7, 30], 6, 64)])
+def test_what_dead_query_rows_hold_does_not_matter(N, n, H, D, dtype):
+    c = Case([300, 40, 700], n, H=H, D=D, Nq=N, dtype=dtype, seed=N).on_device()
+    c.dev_q[(torch.arange(N)[None, :] >= c.n[:, None]).cuda()] = math.nan
+    c.call()
+    torch.cuda.synchronize()
+    c.compare()
+
+
+@pytest.mark.parametrize("over", [0, 1, 2, (0, 1, 2)])
+def test_broadcast_queries(over):
+    c = Case([500, 90], [60, 33], H=8, G=2, seed=3)
+    for d in over if isinstance(over, tuple) else (over,):
+        c.q = c.q.narrow(d, 0, 1).expand(*[c.q.shape[i] if i == d else -1 for i in range(4)])
+    c.on_device()
+    c.dev_q = c.q.cuda()
+    for d in over if isinstance(over, tuple) else (over,):
+        c.dev_q = c.dev_q.narrow(d, 0, 1).expand_as(c.q)
+    assert 0 in c.dev_q.stride()
+    c.call()
+    torch.cuda.synchronize()
+    c.compare()
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3)])
+def test_prefixes_that_no_slot_can_have(window, sinks):
+    """Below 0 counts as 0; behind all pages the rows see every page that is held, or, with a window, the sinks."""
+    c = Case([100, 100, 0], [5, 5, 70], D=64, is_tree=False, window=window, sinks=sinks)
+    c.prefix[0] = 2 ** 31 - 1
+    c.on_device()
+    c.dev_prefix[2] = -7
+    c.call()
+    torch.cuda.synchronize()
+    c.compare(status=[c2t.ST_BAD_PAGE, 0, 0])
+
+
+@pytest.mark.parametrize("N", [1, 3])
+def test_hundreds_of_sequences(N):
+    """More than the thread blocks sum up at once, some without a query."""
+    c = Case([(b * 37) % 200 for b in range(500)], [0 if b % 11 == 3 else N for b in range(500)], H=2, G=1, D=64, is_tree=N > 1, seed=N)
+    c.check()
+
+
+@pytest.mark.parametrize("N,window", [(5, 0), (70, 300)])
+def test_tables_too_wide_for_an_even_deal(N, window):
+    """2^30 tokens a slot: the tiles that there could be are more than 32 bits count, and blocks of rows are then not cut."""
+    B = 16
+    c = Case([9000 if b == 3 else 100 * b for b in range(B)], [N] * B, H=16, G=16, D=64, page=256, window=window, sinks=2, is_tree=window == 0, seed=1)
+    c.on_device()
+    table = torch.full((B, 1 << 22), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table.cuda()
+    c.cache = c2t.KVCache(c.cache.k, c.cache.v, table, c.cache.held, c.cache.refs, q_heads=16, max_queries=N)
+    c.call()
+    torch.cuda.synchronize()
+    c.compare()
