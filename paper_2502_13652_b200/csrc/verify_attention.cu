@@ -113,10 +113,16 @@ struct Params {
   int box_rows;                             // tokens of one copy: a page's, at most a tile's
   int folded;                               // 1: small pages' keys and values come with both halves of a head in one box (one accumulator's blocks)
   int copy_queries;                         // 1: queries come by copies of kQueryRows rows, whole tokens; 0: thread by thread
+  int grid;                                 // thread blocks of the main launch: G
+  int join_step;                            // without a common factor with the other launch's
   int split;                                // 1: tiles are dealt out evenly, blocks of rows may be cut; 0: whole blocks
-  float *part_o;                            // [2 G][kBlockRows][D]: unfinished sums over the values, two per thread block
-  float2 *part_ml;                          // [2 G][kBlockRows]: their maximum (scaled, base 2) and sum of weights
-  int4 *cut;                                // [G]: {pair, key head, first thread block, last} of a cut block of rows
+  // Unfinished rows' sums over the values, two sets per thread block, and their maximum (scaled, base 2) and sum of weights.  Where a sequence has 32 rows at most
+  // they lie side by side, the rows of a copy after those of the other, in a few megabytes: spread over places for 256 rows each, which is tens of megabytes, the
+  // few rows of a single token took X us longer to join.
+  int part_rows, few_rows;                  // places of a set; rows of a sequence, or 0 if they may be more than 32
+  float *part_o;                            // [2 G][D / 4][part_rows][4]
+  float2 *part_ml;                          // [2 G][part_rows]
+  int4 *cut;                                // [G]: {sequence, key head, first row, rows | first thread block << 9 | last << 17} of a cut block of rows
 };
 
 // row -> (new token, query head of the group); rows * group < 2^32, which makes the inverse exact
@@ -369,6 +375,13 @@ __device__ __forceinline__ float larger(float a, float b) {
   return x;
 }
 
+// the largest of a, |b| and |c|, for a >= 0; NaN if any is
+__device__ __forceinline__ float largest_size(float a, float b, float c) {
+  float x;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+  return x;
+}
+
 // logits whose bit is not set become -inf
 __device__ __forceinline__ void mask32(bool masked, uint32_t on, uint32_t *y) {
   if (!masked) return;
@@ -550,7 +563,7 @@ __device__ __noinline__ void once_more(const Params &p, const Block &w, int r, i
     const float x = f == 0.f ? 0.f : o[e] * f;
     if (d < column0 || d >= column0 + columns) continue;
     if (finish) out[d] = from_float<T>(x);
-    else to_part[(d >> 2) * (kBlockRows * 4) + (d & 3)] = x;
+    else to_part[(d >> 2) * (p.part_rows * 4) + (d & 3)] = x;
   }
   __syncwarp();
 }
@@ -578,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     barrier_init(&sh.meet, kSoftmaxThreads);
     barrier_init_fence();
     sh.gave_up = 0;
-    sh.left = 0;
+    sh.left = sh.pair = sh.head = sh.k0 = 0;
     tensor_map_prefetch(&maps.k);
     tensor_map_prefetch(&maps.v);
     if (p.copy_queries) tensor_map_prefetch(&maps.q);
@@ -621,10 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     const bool whole = blocks <= G && sh.most == 0;
     const Deal deal((int)carry * H, G);
     const int begin = whole ? (int)blockIdx.x : deal.begin(blockIdx.x), left = whole ? 0 : deal.begin(blockIdx.x + 1) - begin;
-    if (tid == 0) {
-      sh.left = left;
-      if (whole || left == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    }
+    if (tid == 0) sh.left = left;
     __syncthreads();
 #pragma unroll 1
     for (int pair = tid; pair < n_pairs && (whole || left > 0); pair += kThreads) {
@@ -635,12 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       sh.pair = pair;
       sh.head = head;
       sh.k0 = k0;
-      if (whole) {
-        sh.left = tiles;
-      } else {                              // a block of rows that the thread block before this one began?
-        const int c0 = k0 > 0 ? deal.owner(begin - k0) : -1;
-        p.cut[blockIdx.x] = k0 > 0 && c0 == (int)blockIdx.x - 1 ? make_int4(pair, head, c0, deal.owner(begin - k0 + each - 1)) : make_int4(-1, 0, 0, 0);
-      }
+      if (whole) sh.left = tiles;
     }
   }
   shared_writes_fence();                    // (the ring's copies come where the sums were)
@@ -674,6 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       int left = sh.left, pair = p.split ? sh.pair : 0, head = p.split ? sh.head : blockIdx.x, k0 = p.split ? sh.k0 : 0, known = -1;
       Block w;
       int copied = 0;                       // blocks whose queries were asked for
+      const Deal deal(p.split ? (int)sh.before[n_pairs] * p.c.kv_heads : 0, G);
       for (int i = 0;; ++i) {
         bool more = false;
 #pragma unroll 1
@@ -686,6 +692,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           w.head = head;
           if (p.split && !more) head = p.c.kv_heads;            // to the next pair
           else head += p.split ? 1 : G;
+        }
+        if (i == 0 && p.split) {            // a block of rows that the thread block before this one began?
+          int4 cut = make_int4(0, 0, 0, 0);
+          if (more && k0 > 0) {
+            const int at = deal.begin(blockIdx.x) - k0, c0 = deal.owner(at), c1 = deal.owner(at + w.tiles - 1);
+            if (c0 == (int)blockIdx.x - 1) cut = make_int4(w.b, w.head, w.row0, w.rows | c0 << 9 | c1 << 17);
+          }
+          p.cut[blockIdx.x] = cut;
         }
         w.k0 = k0;
         w.k1 = p.split ? min(w.tiles, k0 + left) : w.tiles;
@@ -1002,59 +1016,82 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         uint32_t *o = reinterpret_cast<uint32_t *>(v);
         __syncwarp();
         tmem_load32((two ? my_o : tmem + 256 + lanes) + c, o);
-        uint32_t o1[32];
-        if (!two) tmem_load32(tmem + 256 + D + lanes + c, o1);
         tmem_wait_loads();
-        bool fine = true;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          v[j] = factor0 == 0.f ? 0.f : v[j] * factor0;
-          if (!two && factor1 != 0.f) v[j] = fmaf(__uint_as_float(o1[j]), factor1, v[j]);
-          fine &= fabsf(v[j]) < INFINITY;
+        for (int j = 0; j < 32; ++j) v[j] *= factor0;
+        if (!two && n > 1) {                // (with one tile the other accumulator holds nothing)
+          uint32_t o1[32];
+          tmem_load32(tmem + 256 + D + lanes + c, o1);
+          tmem_wait_loads();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(o1[j]), factor1, v[j]);
         }
-        return fine;
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) top = largest_size(top, v[j], v[j + 1]);
+        return top < INFINITY;
       };
       // A part: 16 bytes a lane, the rows side by side.  Finished rows go through shared memory, so that they leave in whole sectors and their copies are added
       // up: a warp's 32 rows, 32 columns at a time, 8 vectors a row, swizzled; 4 rows leave at a time, 8 lanes a row.
-      const int place = two ? my_row : row;
+      const int place = two ? my_row : p.few_rows ? (row >> 5) * p.few_rows + my_row : row;
       const int rows_here = two ? 32 : copy_rows / 4, r0 = two ? my_row & ~31 : (warp & 3) * rows_here;         // that this warp writes
       const bool own_rows = two || copy_rows == kRows;          // without copies they are its own, and leave before the next columns come
-      const float *from = two ? stage : reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);            // the warp's, the group's
-      auto write = [&](int c, const float *chunk) {             // 32 columns from c on
-#pragma unroll 2
-        for (int i = 0; i < rows_here; i += 4) {
-          const int r = r0 + i + (lane >> 3), at = two ? r & 31 : r;
-          if (r >= w.rows) break;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      const float *from = reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);         // the group's
+      // (each lane has one row's place, and the others' from their lanes: worked out row by row a block of 256 rows took 8 us here, not XX)
+      const int out_row = own_rows ? my_row : r0 + (lane & (rows_here - 1)), out_node = token_of(p, w.row0 + out_row);
+      const bool to_write = whole && (own_rows || lane < rows_here) && out_row < w.rows;
+      const long long out_at = to_write ? w.b * p.a.out_seq_stride + out_node * p.a.out_token_stride +
+                                              (w.head * p.group + w.row0 + out_row - out_node * p.group) * p.a.out_head_stride : -1;
+      auto write = [&](int c, const float *v) {                 // 32 columns from c on of the warp's own rows: 64 bytes a row, 8 rows leave at a time
+        uint4 *rows16 = reinterpret_cast<uint4 *>(stage);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          rows16[lane * 4 + (j ^ (lane >> 1 & 3))] = make_uint4(pack<T>(v[8 * j], v[8 * j + 1]), pack<T>(v[8 * j + 2], v[8 * j + 3]),
+                                                                pack<T>(v[8 * j + 4], v[8 * j + 5]), pack<T>(v[8 * j + 6], v[8 * j + 7]));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          const int a = i + (lane >> 2);
+          const uint4 x = rows16[a * 4 + ((lane & 3) ^ (a >> 1 & 3))];
+          const long long at = __shfl_sync(~0u, out_at, a);
+          if (at >= 0) *reinterpret_cast<uint4 *>(static_cast<T *>(p.a.out_dev) + at + c + 8 * (lane & 3)) = x;
+        }
+      };
+      auto write_sums = [&](int c, const float *chunk) {        // of the rows whose copies it adds up
 #pragma unroll 1
-          for (int a = at; a < (two ? 32 : kRows); a += two ? 32 : copy_rows) {
-            const float4 x = *reinterpret_cast<const float4 *>(chunk + (a >> 5) * (D * 16) + (a & 31) * 32 + (((lane & 7) ^ (a & 7)) << 2));
-            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        for (int i = 0; i < rows_here; i += 4) {
+          const int r = r0 + i + (lane >> 3);
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int a = r + x * copy_rows;
+            if (a >= kRows) break;
+            const float4 y = *reinterpret_cast<const float4 *>(chunk + (a >> 5) * (D * 16) + (a & 31) * 32 + (((lane & 7) ^ (a & 7)) << 2));
+            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
           }
-          const int node_ = token_of(p, w.row0 + r), head_ = w.head * p.group + w.row0 + r - node_ * p.group;
-          T *out = static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node_ * p.a.out_token_stride + head_ * p.a.out_head_stride;
-          *reinterpret_cast<uint2 *>(out + c + 4 * (lane & 7)) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
+          const long long at = __shfl_sync(~0u, out_at, i + (lane >> 3));
+          if (at >= 0) *reinterpret_cast<uint2 *>(static_cast<T *>(p.a.out_dev) + at + c + 4 * (lane & 7)) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
         }
         __syncwarp();
       };
       if (live && (two || (s == 0 && (!whole || row == my_row)))) {
-        if (!whole) p.part_ml[part * kBlockRows + place] = make_float2(m, l);
+        if (!whole) p.part_ml[part * p.part_rows + place] = make_float2(m, l);
         else if (p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       }
       bool fine = true;
 #pragma unroll 1
       for (int c = 0; c < columns; c += 32) {
-        if (warp_live) {
-          float v[32];
-          fine &= sums(column0 + c, v);
-          float *to = whole ? stage + (own_rows ? 0 : c * 32) + lane * 32 : p.part_o + ((part * (D / 4) + (column0 + c) / 4) * kBlockRows + place) * 4;
+        float v[32];
+        if (warp_live) fine &= sums(column0 + c, v);
+        if (whole && own_rows) {
+          if (warp_live) write(column0 + c, v);
+        } else if (whole ? warp_live : live) {
+          float *to = whole ? stage + c * 32 + lane * 32 : p.part_o + ((part * (D / 4) + (column0 + c) / 4) * p.part_rows + place) * 4;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (whole || live)
-              *reinterpret_cast<float4 *>(to + (whole ? (j ^ (lane & 7)) << 2 : j * (kBlockRows * 4))) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            *reinterpret_cast<float4 *>(to + (whole ? (j ^ (lane & 7)) << 2 : j * (p.part_rows * 4))) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         }
         __syncwarp();
-        if (whole && own_rows) write(column0 + c, from);
       }
       fine |= !live;
       if (whole && !own_rows) {
@@ -1062,7 +1099,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         if (lane == 0) sh.odd[warp] = odd;
         if (!(ok = all_meet())) break;
 #pragma unroll 1
-        for (int c = 0; c < columns; c += 32) write(column0 + c, from + c * 32);
+        for (int c = 0; c < columns; c += 32) write_sums(column0 + c, from + c * 32);
         fine = true;
 #pragma unroll 1
         for (int a = r0 + lane; a < kRows && lane < rows_here; a += copy_rows) fine &= !(sh.odd[s * 4 + (a >> 5)] >> (a & 31) & 1);
@@ -1072,7 +1109,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         // (a lane stands for its own row of the block, or, where there were copies to add up, for one of the rows that the warp wrote)
         const int from_lane = __ffs(again) - 1, r = __shfl_sync(~0u, whole && !own_rows ? r0 + lane : my_row, from_lane), at = __shfl_sync(~0u, place, from_lane);
         once_more<T, D>(p, w, r, whole ? 0 : first_column, whole ? kTile : copy_rows, column0, columns, whole, __shfl_sync(~0u, m, from_lane),
-                        p.part_o + (part * (D / 4) * kBlockRows + at) * 4);
+                        p.part_o + (part * (D / 4) * p.part_rows + at) * 4);
       }
       if (p.copy_queries) {
         shared_writes_fence();
@@ -1089,117 +1126,189 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 
 // ---------------------------------------------------------------- parts of rows that several thread blocks read the keys of
 
-// The parts of a cut block of rows lie with thread blocks c0 .. c1: the first's second place, then the others' first.  Of a part, 16 bytes of all rows lie
+// A cut block of rows.  Its parts lie with thread blocks c0 .. c1: the first's second place, then the others' first.  Of a part, 16 bytes of all rows lie
 // side by side.  Rows that lay in the accumulators in copies have a part for each.
 struct Parts {
   const float *o;
   const float2 *ml;
-  int4 cut;
-  int shift, copy_rows, n;                  // copies = 1 << shift; parts of a row
-  __device__ __forceinline__ Parts(const Params &p, const int4 &cut_, const Block &w) : o(p.part_o), ml(p.part_ml), cut(cut_) {
-    shift = w.rows > kRows ? 0 : w.rows <= 32 ? 2 : w.rows <= 64 ? 1 : 0;
-    copy_rows = kRows >> shift;
-    n = (cut.w - cut.z + 1) << shift;
+  int b, head, row0, rows;
+  int c0, shift, copy_rows, n;              // copies = 1 << shift, so many places apart; parts of a row
+  int places;
+  __device__ __forceinline__ Parts(const Params &p, const int4 &cut) : o(p.part_o), ml(p.part_ml), b(cut.x), head(cut.y), row0(cut.z), rows(cut.w & 511) {
+    c0 = cut.w >> 9 & 255;
+    shift = rows > kRows ? 0 : rows <= 32 ? 2 : rows <= 64 ? 1 : 0;
+    copy_rows = p.few_rows ? p.few_rows : kRows >> shift;
+    places = p.part_rows;
+    n = ((cut.w >> 17) - c0 + 1) << shift;
+    // (a record that is none would lead anywhere)
+    if (rows > kBlockRows || b < 0 || b >= p.c.batch || head < 0 || head >= p.c.kv_heads || row0 < 0 || row0 + (long long)rows > (long long)p.a.max_queries * p.group ||
+        cut.w < 0 || cut.w >> 17 >= p.grid || c0 > cut.w >> 17)
+      rows = 0;
   }
-  __device__ __forceinline__ long long place(int i, int r) const {              // of row r's i-th part among all parts' rows
-    const int c = cut.z + (i >> shift);
-    return (2ll * c + (c == cut.z ? 1 : 0)) * kBlockRows + r + (i & ((1 << shift) - 1)) * copy_rows;
+  __device__ __forceinline__ int set(int i) const {             // of a row's i-th part; and its place there
+    const int c = c0 + (i >> shift);
+    return 2 * c + (c == c0 ? 1 : 0);
   }
-  template <int D>
-  __device__ __forceinline__ const float4 *sums(long long place) const {        // its first 4 columns; the next lie kBlockRows further
-    return reinterpret_cast<const float4 *>(o) + place / kBlockRows * (D / 4 * kBlockRows) + place % kBlockRows;
+  __device__ __forceinline__ int place(int i, int r) const { return r + (i & ((1 << shift) - 1)) * copy_rows; }
+};
+static_assert(kBlockRows < 512, "rows in a cut's description");
+
+// 4 V columns of a row: the running maximum, the sum of weights, the sums over the values.
+template <int V>
+struct Joined {
+  float m = -INFINITY, l = 0.f;
+  float4 o[V];
+  __device__ __forceinline__ Joined() {
+#pragma unroll
+    for (int j = 0; j < V; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void add(const float2 &ml, float top, const float4 *x) {           // top: the maximum of m and ml.x, to which m was raised
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+    l += ml.x == -INFINITY ? ml.y : ml.y * f;                   // (one that sees nothing: 0, or NaN)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      o[j].x = fmaf(x[j].x, f, o[j].x); o[j].y = fmaf(x[j].y, f, o[j].y); o[j].z = fmaf(x[j].z, f, o[j].z); o[j].w = fmaf(x[j].w, f, o[j].w);
+    }
+  }
+  __device__ __forceinline__ void raise(float top) {
+    const float f = m == top || m == -INFINITY ? 1.f : exp2f(m - top);          // (at -inf all sums are 0)
+    l *= f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) { o[j].x *= f; o[j].y *= f; o[j].z *= f; o[j].w *= f; }
+    m = top;
+  }
+  // row r's parts first, first + step, ..: the loads of kAtOnce go out together
+  template <int D, int kAtOnce>
+  __device__ __forceinline__ void parts(const Parts &parts, int r, int first, int step, int vector) {
+#pragma unroll 1
+    for (int i = first; i < parts.n; i += kAtOnce * step) {
+      float2 ml[kAtOnce];
+      float4 x[kAtOnce][V];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int part = min(i + u * step, parts.n - 1), set = parts.set(part), place = parts.place(part, r);
+        ml[u] = parts.ml[set * parts.places + place];
+        const float4 *from = reinterpret_cast<const float4 *>(parts.o) + (set * (D / 4) + vector) * parts.places + place;
+        const bool there = i + u * step < parts.n;
+        if (!there) ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[u][j] = there ? from[j * parts.places] : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) top = fmaxf(top, ml[u].x);
+      raise(top);
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) add(ml[u], top, x[u]);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void write(const Params &p, const Parts &parts, int r, int vector) const {
+    const int at = parts.row0 + r, node = token_of(p, at), h = parts.head * p.group + at - node * p.group;
+    const float share = l == 0.f ? 0.f : 1.f / l;
+    if (vector == 0 && p.a.lse_dev) p.a.lse_dev[((long long)parts.b * p.a.max_queries + node) * p.a.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    T *out = static_cast<T *>(p.a.out_dev) + parts.b * p.a.out_seq_stride + node * p.a.out_token_stride + h * p.a.out_head_stride + vector * 4;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      *reinterpret_cast<uint2 *>(out + 4 * j) = make_uint2(pack<T>(o[j].x * share, o[j].y * share), pack<T>(o[j].z * share, o[j].w * share));
   }
 };
 
-__device__ __forceinline__ float part_factor(const float2 &ml, float m) { return ml.x == -INFINITY ? 0.f : exp2f(ml.x - m); }
-__device__ __forceinline__ float part_sum(const float2 &ml, float f) { return ml.x == -INFINITY ? ml.y : ml.y * f; }   // (one that sees nothing: 0, or NaN)
-
-template <typename T>
-__device__ __forceinline__ T *joined_row(const Params &p, const Block &w, int head, int r, float m, float l, bool tell) {
-  const int at = w.row0 + r, node = token_of(p, at), h = head * p.group + at - node * p.group;
-  if (tell && p.a.lse_dev) p.a.lse_dev[((long long)w.b * p.a.max_queries + node) * p.a.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-  return static_cast<T *>(p.a.out_dev) + w.b * p.a.out_seq_stride + node * p.a.out_token_stride + h * p.a.out_head_stride;
-}
-
-// Grid (G, 32 rows each): a row a lane, D / 8 columns a warp.
-constexpr int kJoinThreads = 256;
-template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(const __grid_constant__ Params p) {
-  chain_enter();
-  const int4 cut = p.cut[blockIdx.x];
-  if (cut.x < 0) return;
-  const Block w = block_of(p, cut.x);
-  const int warp = threadIdx.x >> 5, r = blockIdx.y * 32 + (threadIdx.x & 31);
-  if (r >= w.rows) return;
-  const Parts parts(p, cut, w);
-  constexpr int kVectors = D / 32;          // of 4 columns
-  float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < parts.n; ++i) m = fmaxf(m, parts.ml[parts.place(i, r)].x);
-  float4 o[kVectors];
+// The cut blocks of rows, each with as many items of work as it has groups of `per` rows, summed up.  (A grid over all records that there could be costs more than this:
+// 2400 thread blocks that find nothing to do take 2.6 us longer than 1200.)
+constexpr int kJoinThreads = 256, kJoinBlocks = 4;              // of a multiprocessor
+constexpr int kMaxGrid = 256;               // workspaces are sized without asking the device: at most this many SMs are used
+struct CutList {
+  int4 cut[kMaxGrid];
+  int before[kMaxGrid], warp_sum[kJoinThreads / 32];
+  __device__ __forceinline__ int fill(const Params &p, int per) {               // all threads; how many items there are
+    static_assert(kMaxGrid == kJoinThreads, "a record a thread");
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int4 mine = t < p.grid ? p.cut[t] : make_int4(0, 0, 0, 0);
+    const int items = (Parts(p, mine).rows + per - 1) / per;
+    int x = items;
 #pragma unroll
-  for (int j = 0; j < kVectors; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = 0; i < parts.n; ++i) {
-    const long long place = parts.place(i, r);
-    const float2 ml = parts.ml[place];
-    const float4 *from = parts.sums<D>(place) + warp * kVectors * kBlockRows;
-    const float f = part_factor(ml, m);
-    l += part_sum(ml, f);
-#pragma unroll
-    for (int j = 0; j < kVectors; ++j) {
-      const float4 x = from[j * kBlockRows];
-      o[j].x = fmaf(x.x, f, o[j].x); o[j].y = fmaf(x.y, f, o[j].y); o[j].z = fmaf(x.z, f, o[j].z); o[j].w = fmaf(x.w, f, o[j].w);
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(~0u, x, d);
+      if (lane >= d) x += y;
     }
-  }
-  const float share = l == 0.f ? 0.f : 1.f / l;
-  T *out = joined_row<T>(p, w, cut.y, r, m, l, warp == 0) + warp * (D / 8);
+    cut[t] = mine;
+    if (lane == 31) warp_sum[warp] = x;
+    __syncthreads();
+    int earlier = 0, all = 0;
 #pragma unroll
-  for (int j = 0; j < kVectors; ++j)
-    *reinterpret_cast<uint2 *>(out + 4 * j) = make_uint2(pack<T>(o[j].x * share, o[j].y * share), pack<T>(o[j].z * share, o[j].w * share));
+    for (int w = 0; w < kJoinThreads / 32; ++w) {
+      const int s = warp_sum[w];
+      earlier += w < warp ? s : 0;
+      all += s;
+    }
+    before[t] = earlier + x - items;
+    __syncthreads();
+    return all;
+  }
+  __device__ __forceinline__ int find(int item) const {         // the record whose item it is: the last with no more items before it
+    int at = 0;
+#pragma unroll
+    for (int step = kMaxGrid / 2; step > 0; step >>= 1)
+      if (before[at + step] <= item) at += step;
+    return at;
+  }
+};
+
+// Thread blocks with numbers side by side often come to one multiprocessor, the first that has room: few items go to numbers far apart.  (A token of 32 heads
+// behind 3000 others takes 18 us so, 28 with item i in thread block i.)
+__device__ __forceinline__ int first_item(const Params &p) { return (int)(blockIdx.x * (unsigned)p.join_step % gridDim.x); }
+
+// An item: 32 rows, half the columns; a row a lane, D / 16 columns a warp.
+template <typename T, int D>
+__global__ void __launch_bounds__(kJoinThreads, kJoinBlocks) join_parts_kernel(const __grid_constant__ Params p) {
+  chain_enter();
+  __shared__ CutList list;
+  const int items = 2 * list.fill(p, 32);
+  constexpr int kVectors = D / 64;          // of 4 columns
+#pragma unroll 1
+  for (int item = first_item(p); item < items; item += gridDim.x) {
+    const int at = list.find(item >> 1), r = ((item >> 1) - list.before[at]) * 32 + (threadIdx.x & 31);
+    const Parts parts(p, list.cut[at]);
+    if (r >= parts.rows) continue;
+    const int vector = ((item & 1) * (kJoinThreads / 32) + (threadIdx.x >> 5)) * kVectors;
+    Joined<kVectors> sum;
+    sum.template parts<D, 4>(parts, r, 0, 1, vector);
+    sum.template write<T>(p, parts, r, vector);
+  }
 }
 
-// Grid (G, rows): few rows have many parts each (copies too), which one after the other are what the launch would wait for.  A row a block, every so
-// many-th part a group of D / 4 lanes, 4 columns a lane.
+// Few rows have many parts each (copies too), which one after the other are what the launch would wait for.  An item is a row, every so many-th part a
+// group of D / 4 lanes', 4 columns a lane.
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) join_few_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kJoinThreads, kJoinBlocks) join_few_kernel(const __grid_constant__ Params p) {
   chain_enter();
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  __shared__ CutList list;
   __shared__ float4 sums[kGroups][kLanes];
-  __shared__ float total[kGroups];
-  const int4 cut = p.cut[blockIdx.x];
-  if (cut.x < 0) return;
-  const Block w = block_of(p, cut.x);
-  const int r = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x / kLanes, column = threadIdx.x % kLanes;
-  if (r >= w.rows) return;
-  const Parts parts(p, cut, w);
-  float m = -INFINITY, l = 0.f;
-  for (int i = lane; i < parts.n; i += 32) m = fmaxf(m, parts.ml[parts.place(i, r)].x);
+  __shared__ float2 ml[kGroups];
+  const int items = list.fill(p, 1);
+  const int group = threadIdx.x / kLanes, column = threadIdx.x % kLanes;
+#pragma unroll 1
+  for (int item = first_item(p); item < items; item += gridDim.x) {
+    const int at = list.find(item), r = item - list.before[at];
+    const Parts parts(p, list.cut[at]);
+    Joined<1> sum;
+    sum.template parts<D, 4>(parts, r, group, kGroups, column);
+    sums[group][column] = sum.o[0];
+    if (column == 0) ml[group] = make_float2(sum.m, sum.l);
+    __syncthreads();
+    if (group == 0) {
+      float top = sum.m;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = group; i < parts.n; i += kGroups) {
-    const long long place = parts.place(i, r);
-    const float2 ml = parts.ml[place];
-    const float4 x = parts.sums<D>(place)[column * kBlockRows];
-    const float f = part_factor(ml, m);
-    l += part_sum(ml, f);
-    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
-  }
-  sums[group][column] = o;
-  if (column == 0) total[group] = l;
-  __syncthreads();
-  if (group > 0) return;
+      for (int g = 1; g < kGroups; ++g) top = fmaxf(top, ml[g].x);
+      sum.raise(top);
 #pragma unroll
-  for (int g = 1; g < kGroups; ++g) {
-    const float4 x = sums[g][column];
-    o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-    l = g == 1 ? total[0] + total[1] : l + total[g];
+      for (int g = 1; g < kGroups; ++g) sum.add(ml[g], top, &sums[g][column]);
+      sum.template write<T>(p, parts, r, column);
+    }
+    __syncthreads();
   }
-  const float share = l == 0.f ? 0.f : 1.f / l;
-  T *out = joined_row<T>(p, w, cut.y, r, m, l, column == 0) + 4 * column;
-  *reinterpret_cast<uint2 *>(out) = make_uint2(pack<T>(o.x * share, o.y * share), pack<T>(o.z * share, o.w * share));
 }
 
 int check_attention(const c2t_cache *c, const c2t_attention *a) {
@@ -1283,7 +1392,10 @@ bool encode_queries(const c2t_cache &c, const c2t_attention &a, int group, Tenso
                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kMaxGrid = 256;               // workspaces are sized without asking the device: at most this many SMs are used
+int common_factor(int a, int b) {
+  while (b != 0) { const int r = a % b; a = b; b = r; }
+  return a;
+}
 
 struct Workspace { size_t o, ml, cut, bytes; };
 
@@ -1304,9 +1416,8 @@ cudaError_t launch_attention(const Params &p, const Maps &maps, int sms, cudaStr
   if (e == cudaSuccess) e = launch_chained(attend_tiles_kernel<T, D>, dim3(sms), dim3(kThreads), smem, s, maps, p);
   if (e == cudaSuccess && p.split) {
     const long long rows = (long long)p.a.max_queries * p.group;
-    const int most = (int)(rows < kBlockRows ? rows : kBlockRows);
-    if (most <= 32) e = launch_chained(join_few_kernel<T, D>, dim3(sms, most), dim3(kJoinThreads), 0, s, p);
-    else e = launch_chained(join_parts_kernel<T, D>, dim3(sms, (most + 31) / 32), dim3(kJoinThreads), 0, s, p);
+    if (rows <= 32) e = launch_chained(join_few_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
+    else e = launch_chained(join_parts_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
   }
   return e;
 }
@@ -1360,6 +1471,11 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.folded = p.c.head_dim == 128 && p.c.page_size <= 16 && encode_folded(p.c, p.c.k_dev, p.a.layer, &maps.k_folded) &&
              encode_folded(p.c, p.c.v_dev, p.a.layer, &maps.v_folded);
   if (sms > kMaxGrid) sms = kMaxGrid;
+  p.grid = sms;
+  p.few_rows = rows <= 32 ? (int)rows : 0;
+  p.part_rows = rows <= 32 ? 4 * (int)rows : rows <= kRows ? kRows : kBlockRows;
+  p.join_step = kJoinBlocks * sms * 309 / 500 | 1;              // (the golden section: multiples of it keep apart)
+  while (common_factor(p.join_step, kJoinBlocks * sms) != 1) p.join_step += 2;
   const bool bf16 = p.c.dtype == C2T_BF16;
   auto launch = p.c.head_dim == 64 ? (bf16 ? launch_attention<__nv_bfloat16, 64> : launch_attention<__half, 64>)
                                    : (bf16 ? launch_attention<__nv_bfloat16, 128> : launch_attention<__half, 128>);
