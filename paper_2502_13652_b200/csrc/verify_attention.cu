@@ -115,7 +115,8 @@ struct Params {
   int copy_queries;                         // 1: queries come by copies of kQueryRows rows, whole tokens; 0: thread by thread
   int grid;                                 // thread blocks of the main launch: G
   int join_step;                            // without a common factor with the other launch's
-  int split;                                // 1: tiles are dealt out evenly, blocks of rows may be cut; 0: whole blocks
+  int split;                                // 1: blocks of rows may be cut; 0: whole ones
+  int least_tiles, more_tiles;              // of a piece, where all get equal ones, and how many more than an even deal they may have
   // Unfinished rows' sums over the values, two sets per thread block, and their maximum (scaled, base 2) and sum of weights.  Where a sequence has 32 rows at most
   // they lie side by side, the rows of a copy after those of the other, in a few megabytes: spread over places for 256 rows each, which is tens of megabytes, the
   // few rows of a single token took X us longer to join.
@@ -227,11 +228,10 @@ struct alignas(1024) Shared {
   int gave_up;
   uint32_t odd[8];
   long long warp_sum[kThreads / 32];
-  int most, left, pair, head, k0;
+  int left, pair, head, k0, c0, c1, long_ones;
 };
 
 constexpr int kMaxPairs = C2T_MAX_BATCH;    // for an even deal
-constexpr int kWholeTiles = 2;              // of a block of rows that is not cut where every one finds a thread block
 
 template <int D>
 __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
@@ -592,10 +592,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     barrier_init_fence();
     sh.gave_up = 0;
     sh.left = sh.pair = sh.head = sh.k0 = 0;
+    sh.c0 = -1;
+    sh.long_ones = 0;
     tensor_map_prefetch(&maps.k);
     tensor_map_prefetch(&maps.v);
     if (p.copy_queries) tensor_map_prefetch(&maps.q);
-    sh.most = 0;
   }
   chain_wait();
 
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     for (int base = 0; base < n_pairs; base += kThreads) {
       const int pair = base + tid, tiles = pair < n_pairs ? block_of(p, pair).tiles : 0;
       const long long mine = (tiles > 0 ? 1ll << 32 : 0) + tiles;
-      if (tiles > kWholeTiles) sh.most = tiles;                 // (any of those)
+      if (tiles > p.least_tiles) sh.long_ones = 1;
       long long x = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -629,23 +630,62 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     }
     if (tid == 0) sh.before[n_pairs] = carry;
     __syncthreads();
-    // Few short blocks of rows go to a thread block each, uncut: adding up parts takes longer than the tiles do.
-    const int H = p.c.kv_heads, blocks = (int)(carry >> 32) * H;
-    const bool whole = blocks <= G && sh.most == 0;
-    const Deal deal((int)carry * H, G);
-    const int begin = whole ? (int)blockIdx.x : deal.begin(blockIdx.x), left = whole ? 0 : deal.begin(blockIdx.x + 1) - begin;
-    if (tid == 0) sh.left = left;
-    __syncthreads();
+    auto tiles_of = [&](int pair) { return (int)sh.before[pair + 1] - (int)sh.before[pair]; };
+    const int H = p.c.kv_heads, total = (int)carry * H, blocks = (int)(carry >> 32) * H;
+    // Where every block of rows finds a thread block: equal pieces of each, of so few tiles that every piece finds one.  Each warp tries a number of tiles.
+    int piece = 0;
+    if (blocks <= G && !sh.long_ones) {
+      piece = p.least_tiles;                // (no block of rows has more)
+    } else if (blocks <= G) {
+      const int least = max((total + G - 1) / G, p.least_tiles);
+      int pieces = 0;
+      if (warp <= p.more_tiles)
 #pragma unroll 1
-    for (int pair = tid; pair < n_pairs && (whole || left > 0); pair += kThreads) {
-      const int tiles = (int)sh.before[pair + 1] - (int)sh.before[pair], each = whole ? (tiles > 0) : tiles;      // of a head
-      const int first = (whole ? (int)(sh.before[pair] >> 32) : (int)sh.before[pair]) * H;
-      if (begin < first || begin >= first + each * H) continue;                 // (one pair of one thread, or none)
-      const int head = (begin - first) / each, k0 = begin - first - head * each;
-      sh.pair = pair;
-      sh.head = head;
-      sh.k0 = k0;
-      if (whole) sh.left = tiles;
+        for (int pair = lane; pair < n_pairs; pair += 32) pieces += (tiles_of(pair) + least + warp - 1) / (least + warp);
+      pieces = __reduce_add_sync(~0u, pieces) * H;
+      if (lane == 0) sh.warp_sum[warp] = pieces;
+      __syncthreads();
+#pragma unroll 1
+      for (int w = p.more_tiles; w >= 0; --w)
+        if (sh.warp_sum[w] <= G) piece = least + w;
+    }
+    // c0, c1: of a block of rows that the thread block before this one began, the first and the last thread block
+    auto found = [&](int pair, int head, int k0, int left, int c0, int c1) {    // (by one thread, or none)
+      sh.pair = pair; sh.head = head; sh.k0 = k0; sh.left = left; sh.c0 = c0; sh.c1 = c1;
+    };
+    const int me = blockIdx.x;
+    if (piece > 0) {
+      if (warp == 0) {
+        int before = 0;                     // pieces
+#pragma unroll 1
+        for (int base = 0; base < n_pairs && before <= me; base += 32) {
+          const int pair = base + lane, tiles = pair < n_pairs ? tiles_of(pair) : 0, each = (tiles + piece - 1) / piece;          // of a head
+          int x = each * H;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(~0u, x, d);
+            if (lane >= d) x += y;
+          }
+          const int first = before + x - each * H;
+          if (me >= first && me < before + x) {
+            const int head = (me - first) / each, at = me - first - head * each;
+            const int k0 = (unsigned)at * tiles / each;         // (256 thread blocks, 2^23 tiles)
+            found(pair, head, k0, (int)((at + 1u) * tiles / each) - k0, at == 1 ? me - 1 : -1, me + each - 2);
+          }
+          before += __shfl_sync(~0u, x, 31);
+        }
+      }
+    } else {
+      const Deal deal(total, G);
+      const int begin = deal.begin(me), left = deal.begin(me + 1) - begin;
+#pragma unroll 1
+      for (int pair = tid; pair < n_pairs && left > 0; pair += kThreads) {
+        const int each = tiles_of(pair), first = (int)sh.before[pair] * H;
+        if (begin < first || begin >= first + each * H) continue;
+        const int head = (begin - first) / each, k0 = begin - first - head * each;
+        const bool second = k0 > 0 && deal.owner(begin - k0) == me - 1;
+        found(pair, head, k0, left, second ? me - 1 : -1, second ? deal.owner(begin - k0 + each - 1) : 0);
+      }
     }
   }
   shared_writes_fence();                    // (the ring's copies come where the sums were)
@@ -679,7 +719,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       int left = sh.left, pair = p.split ? sh.pair : 0, head = p.split ? sh.head : blockIdx.x, k0 = p.split ? sh.k0 : 0, known = -1;
       Block w;
       int copied = 0;                       // blocks whose queries were asked for
-      const Deal deal(p.split ? (int)sh.before[n_pairs] * p.c.kv_heads : 0, G);
       for (int i = 0;; ++i) {
         bool more = false;
 #pragma unroll 1
@@ -693,14 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           if (p.split && !more) head = p.c.kv_heads;            // to the next pair
           else head += p.split ? 1 : G;
         }
-        if (i == 0 && p.split) {            // a block of rows that the thread block before this one began?
-          int4 cut = make_int4(0, 0, 0, 0);
-          if (more && k0 > 0) {
-            const int at = deal.begin(blockIdx.x) - k0, c0 = deal.owner(at), c1 = deal.owner(at + w.tiles - 1);
-            if (c0 == (int)blockIdx.x - 1) cut = make_int4(w.b, w.head, w.row0, w.rows | c0 << 9 | c1 << 17);
-          }
-          p.cut[blockIdx.x] = cut;
-        }
+        if (i == 0 && p.split) p.cut[blockIdx.x] = more && sh.c0 >= 0 ? make_int4(w.b, w.head, w.row0, w.rows | sh.c0 << 9 | sh.c1 << 17) : make_int4(0, 0, 0, 0);
         w.k0 = k0;
         w.k1 = p.split ? min(w.tiles, k0 + left) : w.tiles;
         left -= w.k1 - k0;
@@ -1452,6 +1484,10 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.box_rows = p.c.page_size < kTile ? p.c.page_size : kTile;
   // (tiles of all blocks of rows are counted in 32 bits)
   p.split = blocks * p.c.batch <= kMaxPairs && blocks * p.c.batch * p.c.kv_heads * ((int64_t)p.c.max_pages * p.c.page_size / kTile + 1) <= 0x7FFFFFFF;
+  // Equal pieces against an even deal: 8 trees of 60 nodes, 32 heads, behind 2048 tokens take 38.8 us and 41.2, a token of 32
+  // heads behind 6000 others 17.0 and 20.5.  A piece of fewer tiles than these costs more to join than it saves: 8 such trees behind 300 take 23.7 us with pieces of 2 tiles, 20.2 of 3.
+  p.least_tiles = rows > kRows ? 3 : 2;
+  p.more_tiles = rows > kRows ? 3 : 4;
   char *base = static_cast<char *>(workspace_dev);
   p.part_o = reinterpret_cast<float *>(base + at.o);
   p.part_ml = reinterpret_cast<float2 *>(base + at.ml);
