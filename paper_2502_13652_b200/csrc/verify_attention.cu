@@ -99,7 +99,9 @@ __device__ void attend_row(const c2t_cache &c, const c2t_attention &a, const Sig
 // ---------------------------------------------------------------- the blocks of work
 // The rows of a sequence and a key head are (new token, query head of the group), token-major; 256 of them, or what is left of a
 // sequence, form a block of rows.  Its keys are cut into tiles of 128: those that hold the sinks, then those from the first key that a
-// row's window can reach.  All of it follows from the lengths on the device.
+// row's window can reach.  All of it follows from the lengths on the device.  A thread block per multiprocessor takes its share of all tiles: equal
+// pieces of the blocks of rows where there are few of them, else an even deal, which cuts blocks wherever a share ends.  Rows of a cut block leave as parts
+// for a second launch to add up.
 
 constexpr int kTile = 128;                  // keys of a tile
 constexpr int kRows = 128;                  // rows of one accumulator
@@ -119,7 +121,7 @@ struct Params {
   int least_tiles, more_tiles;              // of a piece, where all get equal ones, and how many more than an even deal they may have
   // Unfinished rows' sums over the values, two sets per thread block, and their maximum (scaled, base 2) and sum of weights.  Where a sequence has 32 rows at most
   // they lie side by side, the rows of a copy after those of the other, in a few megabytes: spread over places for 256 rows each, which is tens of megabytes, the
-  // few rows of a single token took X us longer to join.
+  // few rows of a single token behind 3000 others took 5 us longer to join.
   int part_rows, few_rows;                  // places of a set; rows of a sequence, or 0 if they may be more than 32
   float *part_o;                            // [2 G][D / 4][part_rows][4]
   float2 *part_ml;                          // [2 G][part_rows]
@@ -203,7 +205,9 @@ struct Deal {
 constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x D; P in the place of S, with heads of 64 in columns of its own
 template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 14.f : 40.f;
-constexpr int kProducts = 1;                // of 8 powers of two that are not taken by the special-function unit: 2 kProducts / 2
+// Of 16 powers of two, 2 kProducts are products and sums instead of the special-function unit's.  64 sequences' tokens behind 4096: 136 us with 1, 139 with 0, 136 with 2;
+// trees of 8 x 2048 38.8, 39.6, 38.9; of 1 x 16000 53.4, 52.6, 53.7; a chunk of 2 x 2048 behind 6000 452, 452, 461.
+constexpr int kProducts = 1;
 constexpr int kTries = 1 << 20;             // of a wait, 3900 cycles each: after two seconds the block gives up
 
 template <int D> __device__ __forceinline__ constexpr int weights_at(int s) { return D == 64 ? 384 + s * 64 : s * kTile; }
@@ -276,7 +280,7 @@ __device__ __forceinline__ int shift_of_last_box(int there, int box_rows) {
   return there >= kTile || there <= 0 ? 0 : last_box(there, box_rows) + box_rows - there;
 }
 
-// rows of one of the copies of a block's rows
+// rows of one of the copies of a block's rows: four of up to 32, two of up to 64
 __device__ __forceinline__ int rows_of_copy(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : kRows; }
 
 // Do the columns of such a block's tiles take their keys from folded pages of 16, 8 of every page after the other 8?
@@ -1063,13 +1067,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         for (int j = 0; j < 32; j += 2) top = largest_size(top, v[j], v[j + 1]);
         return top < INFINITY;
       };
-      // A part: 16 bytes a lane, the rows side by side.  Finished rows go through shared memory, so that they leave in whole sectors and their copies are added
-      // up: a warp's 32 rows, 32 columns at a time, 8 vectors a row, swizzled; 4 rows leave at a time, 8 lanes a row.
+      // A part: 16 bytes a lane, the rows side by side.  Finished rows go through shared memory, so that they leave in whole sectors: a warp's own 32 rows as 16-bit
+      // numbers, 32 columns at a time, swizzled, or, where there are copies to add up, all of their columns in 32 bits.
       const int place = two ? my_row : p.few_rows ? (row >> 5) * p.few_rows + my_row : row;
       const int rows_here = two ? 32 : copy_rows / 4, r0 = two ? my_row & ~31 : (warp & 3) * rows_here;         // that this warp writes
       const bool own_rows = two || copy_rows == kRows;          // without copies they are its own, and leave before the next columns come
       const float *from = reinterpret_cast<const float *>(sh.q[0]) + s * 4 * (D * 16);         // the group's
-      // (each lane has one row's place, and the others' from their lanes: worked out row by row a block of 256 rows took 8 us here, not XX)
+      // (each lane has one row's place, and the others' from their lanes: worked out row by row a block of 256 rows took 8 us here, not 3)
       const int out_row = own_rows ? my_row : r0 + (lane & (rows_here - 1)), out_node = token_of(p, w.row0 + out_row);
       const bool to_write = whole && (own_rows || lane < rows_here) && out_row < w.rows;
       const long long out_at = to_write ? w.b * p.a.out_seq_stride + out_node * p.a.out_token_stride +
@@ -1448,6 +1452,7 @@ cudaError_t launch_attention(const Params &p, const Maps &maps, int sms, cudaStr
   if (e == cudaSuccess) e = launch_chained(attend_tiles_kernel<T, D>, dim3(sms), dim3(kThreads), smem, s, maps, p);
   if (e == cudaSuccess && p.split) {
     const long long rows = (long long)p.a.max_queries * p.group;
+    // (a token of 32 heads behind 6000 others: 17.0 us with the first, 29.8 with the second)
     if (rows <= 32) e = launch_chained(join_few_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
     else e = launch_chained(join_parts_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
   }
@@ -1482,7 +1487,7 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.group_inverse = p.group > 1 ? (uint32_t)((0x100000000ull + p.group - 1) / p.group) : 0;
   p.blocks_per_seq = (int)blocks;
   p.box_rows = p.c.page_size < kTile ? p.c.page_size : kTile;
-  // (tiles of all blocks of rows are counted in 32 bits)
+  // (tiles of all blocks of rows are counted in 32 bits; with whole blocks 64 sequences' tokens behind 4096 in pages of 16 take 184 us instead of 153)
   p.split = blocks * p.c.batch <= kMaxPairs && blocks * p.c.batch * p.c.kv_heads * ((int64_t)p.c.max_pages * p.c.page_size / kTile + 1) <= 0x7FFFFFFF;
   // Equal pieces against an even deal: 8 trees of 60 nodes, 32 heads, behind 2048 tokens take 38.8 us and 41.2, a token of 32
   // heads behind 6000 others 17.0 and 20.5.  A piece of fewer tiles than these costs more to join than it saves: 8 such trees behind 300 take 23.7 us with pieces of 2 tiles, 20.2 of 3.
@@ -1499,11 +1504,13 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
     cudaGetLastError();
     return C2T_ECUDA;
   }
-  // groups of heads that divide a copy's rows; no dimension without a stride, as broadcast queries have
+  // By copies where the groups of heads divide a copy's rows and no dimension is without a stride, as broadcast queries have: windows of 1024, 16 sequences of 64
+  // heads, take 75.6 us, thread by thread 79.1; trees of 32 x 3000 121.5 and 124.2; a chunk 452 and 453.
   const bool strides = (p.c.batch == 1 || p.a.q_seq_stride > 0) && (p.a.max_queries == 1 || p.a.q_token_stride > 0) && (p.a.q_heads == 1 || p.a.q_head_stride > 0);
   p.copy_queries = strides && p.group <= kQueryRows && (p.group & (p.group - 1)) == 0 && encode_queries(p.c, p.a, p.group, &maps.q);
-  // Copies of 2 KB are dealt with at 140 cycles each, which is less than the memory gives; with both halves of a head in one, pages of 16 tokens cost
-  // (two products for the logits of half the columns each, which do not matter where the copies do) ...
+  // Copies of 2 KB are dealt with at 140 cycles each, which is less than the memory gives.  With both halves of a head in one, 64 sequences' tokens behind 4096 in
+  // pages of 16 take 152 us instead of 185, trees of 32 x 3000 256 instead of 291.  (The logits are two products of half the columns each then, which blocks of
+  // more than 128 rows would wait for: they take pages half by half.)
   p.folded = p.c.head_dim == 128 && p.c.page_size <= 16 && encode_folded(p.c, p.c.k_dev, p.a.layer, &maps.k_folded) &&
              encode_folded(p.c, p.c.v_dev, p.a.layer, &maps.v_folded);
   if (sms > kMaxGrid) sms = kMaxGrid;
