@@ -378,3 +378,41 @@ def test_tables_too_wide_for_an_even_deal(N, window):
     c.call()
     torch.cuda.synchronize()
     c.compare()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [1, 5, 24, 32, 33, 48, 64, 65, 128, 129, 256, 300])
+def test_rows_whose_keys_several_thread_blocks_read(rows, D):
+    """Every way in which parts of rows lie and are joined, with sequences that have fewer rows than the call allows."""
+    Case([4000, 130, 2500, 0], [rows, max(rows // 2, 1), 1, rows], H=2, G=2, D=D, is_tree=rows % 2 == 0, seed=rows).check()
+
+
+@pytest.mark.parametrize("B,H,G,N,prefix", [(3, 4, 4, 5, 2000), (2, 8, 2, 60, 1000), (9, 16, 16, 1, 700), (37, 4, 4, 2, 300), (38, 4, 4, 2, 300), (5, 24, 8, 9, 4500)])
+def test_pieces_and_even_deals(B, H, G, N, prefix):
+    """Fewer blocks of rows than thread blocks, as many (148) and more, of unequal lengths."""
+    Case([prefix * (b + 1) // B for b in range(B)], [N] * B, H=H, G=G, D=64, is_tree=N > 2, seed=B).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,H", [(1, 2), (3, 6), (60, 2), (140, 4)])
+def test_numbers_that_are_none_behind_a_window_in_a_part(N, H, dtype):
+    """The key just behind the first row's window lies in a tile that is read, by a thread block that has a part of the rows."""
+    c = Case([3000, 5000], [N, N], H=H, G=2, D=64, is_tree=False, window=1000, dtype=dtype, seed=N)
+    for b, p in enumerate((2000, 4000)):
+        for t in (c.k, c.v):
+            t[0, int(c.table[b, p // 16]), p % 16] = math.nan
+    c.check()
+
+
+def test_two_streams_with_a_workspace_each():
+    a = Case([3000, 10], [60, 60], H=8, G=2, seed=1).on_device()
+    b = Case([40, 2500], [12, 60], H=8, G=2, seed=2).on_device()
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s in zip((a, b), sides):
+            with torch.cuda.stream(s):
+                c.call()
+    torch.cuda.synchronize()
+    a.compare()
+    b.compare()
