@@ -1026,18 +1026,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         sh.ml[s][row] = make_float2(m, l);
         if (!(ok = all_meet())) break;
         const int lane_row = whole ? my_row : row, step = whole ? copy_rows : kRows;
+        float2 e[4][2];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) e[x][v] = lane_row + x * step < kRows ? sh.ml[v][lane_row + x * step] : make_float2(-INFINITY, 0.f);
         m = -INFINITY;
-#pragma unroll 1
-        for (int i = lane_row; i < kRows; i += step) m = fmaxf(m, fmaxf(sh.ml[0][i].x, sh.ml[1][i].x));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) m = fmaxf(m, fmaxf(e[x][0].x, e[x][1].x));
         l = 0.f;
-#pragma unroll 1
-        for (int i = lane_row; i < kRows; i += step)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            const float2 e = sh.ml[v][i];
-            const float f = e.x == -INFINITY ? 0.f : exp2_fast(e.x - m);
-            l += e.x == -INFINITY ? e.y : e.y * f;              // (0, or NaN)
-            if (i == row) { if (v == 0) factor0 = f; else factor1 = f; }
+            const float f = e[x][v].x == -INFINITY ? 0.f : exp2_fast(e[x][v].x - m);
+            l += e[x][v].x == -INFINITY ? e[x][v].y : e[x][v].y * f;            // (0, or NaN)
+            if (lane_row + x * step == row) { if (v == 0) factor0 = f; else factor1 = f; }
           }
       }
       const float share = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
@@ -1095,7 +1099,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       };
       auto write_sums = [&](int c, const float *chunk) {        // of the rows whose copies it adds up
 #pragma unroll 1
-        for (int i = 0; i < rows_here; i += 4) {
+        for (int i = 0; i < rows_here && r0 + i < w.rows; i += 4) {
           const int r = r0 + i + (lane >> 3);
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -1121,7 +1125,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         if (warp_live) fine &= sums(column0 + c, v);
         if (whole && own_rows) {
           if (warp_live) write(column0 + c, v);
-        } else if (whole ? warp_live : live) {
+        } else if (live) {
           float *to = whole ? stage + c * 32 + lane * 32 : p.part_o + ((part * (D / 4) + (column0 + c) / 4) * p.part_rows + place) * 4;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
