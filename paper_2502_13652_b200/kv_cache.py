@@ -68,9 +68,10 @@ def _calls() -> C.CDLL:
 
 
 # The calls are short on the device, so their arguments are marshalled with as few steps as the checks allow: the structures of a call are
-# packed in one step (native alignment gives C's layout; a test compares it with the ctypes structures above).
-_ATTENTION = struct.Struct("@iiiPPqqqqqqPPPPiPiif")
-_RULES = struct.Struct("@iiiiPPqqqqPPqPPPPqPqqiPPP")
+# packed in one step (native alignment gives C's layout, "0P" the padding at its end, which the library copies too; a test compares it with
+# the ctypes structures above).
+_ATTENTION = struct.Struct("@iiiPPqqqqqqPPPPiPiif0P")
+_RULES = struct.Struct("@iiiiPPqqqqPPqPPPPqPqqiPPP0P")
 _int32, _float32, _int64 = torch.int32, torch.float32, torch.int64
 
 

@@ -151,3 +151,10 @@ def test_rows_in_one_place_are_refused(L, what):
 def test_counts_of_more_entries_than_32_bits_reach(L):
     n = (1 << 30) + 1
     assert L.c2t_count_tokens(A, 1000, 2, 1000, A, n, None, 0, A, 0, n, 1, None) == c2t.ERANGE
+
+
+def test_packed_structures_are_as_long_as_those_of_c():
+    """The library copies whole structures: a buffer that ends with the last field is too short for one that ends in padding."""
+    from paper_2502_13652_b200 import kv_cache as K
+    assert K._ATTENTION.size == C.sizeof(c2t_attention)
+    assert K._RULES.size == C.sizeof(c2t_logit_rules)
