@@ -491,8 +491,9 @@ int c2t_decode_step_host(c2t_ctx *ctx, const c2t_host_step *io, void *stream);
  * A page holds page_size tokens of all layers and heads; position p of slot b lies in page table[b][p / page_size], place
  * p % page_size.  refs counts the slots that hold a page: 0 = free.  Free pages are always taken in ascending order, for the slots in
  * ascending order, so that equal calls leave equal tables.  A fresh cache is: refs 0, held 0, status 0; the library
- * never reads entries of table at or past held.  Pages below a fork's length are shared by the slots that hold them; whoever
- * writes at or past its own length therefore writes to pages that nobody else holds.
+ * never reads entries of table at or past held.  Whole pages below a fork's length are shared by the slots that hold them, and no call writes to a page
+ * whose count is above 1: that place counts as one without a page.  A slot that only grows never meets one.  One that is released to a length inside a shared
+ * page and is to go on from there forks its tokens into an empty slot (c2t_cache_fork copies the begun page) and gives its own pages back.
  * Calls on one cache must be ordered (one stream, or events), as those of a context.
  */
 #define C2T_MAX_PAGE_SIZE 256
@@ -540,8 +541,8 @@ int c2t_cache_fork(const c2t_cache *cache, const int32_t *src_dev, const int32_t
 /*
  * Writes the keys and values of new tokens to their pages: token j < count_dev[b] of slot b goes to position start_dev[b] + j of
  * `layer`.  k_new_dev / v_new_dev: [B, max_new, kv_heads, head_dim] of the cache's dtype, element offset b*seq_stride + j*token_stride +
- * h*head_stride + d (16-byte aligned, as in c2t_cache).  A token whose position has no held page is skipped and sets
- * C2T_ST_BAD_PAGE.  One launch.
+ * h*head_stride + d (16-byte aligned, as in c2t_cache).  A token whose position has no held page, or one that another slot holds too,
+ * is skipped and sets C2T_ST_BAD_PAGE.  One launch.
  */
 int c2t_cache_append(const c2t_cache *cache, int32_t layer, const void *k_new_dev, const void *v_new_dev, int32_t max_new,
                      int64_t seq_stride, int64_t token_stride, int64_t head_stride, const int32_t *start_dev,
@@ -552,7 +553,7 @@ int c2t_cache_append(const c2t_cache *cache, int32_t layer, const void *k_new_de
  * prefix_len[b] + path[b][d] move to prefix_len[b] + d, d = 0 .. accept_len[b].  accept_len_dev [B] and path_dev [B, path_width]
  * as c2t_accept writes them (node ids ascending along the path; path_width = D + 1, at most C2T_MAX_DEPTH + 1).
  * new_len_dev [B] (an array of its own, may be NULL): prefix_len + accept_len + 1, the next step's prefix and what c2t_cache_release wants.  A path that is not
- * ascending, or leaves the held pages, sets C2T_ST_BAD_PAGE; that slot is left as it was and new_len is its prefix_len.  One launch.
+ * ascending, leaves the held pages, or would move a node into a page that another slot holds too, sets C2T_ST_BAD_PAGE; that slot is left as it was and new_len is its prefix_len.  One launch.
  */
 int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, const int32_t *accept_len_dev,
                       const int32_t *path_dev, int32_t path_width, int32_t *new_len_dev, void *stream);

@@ -32,14 +32,22 @@ constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kFirstScan = 4, kScan = 16;   // counts per lane and round of the search for free pages
 constexpr int kCopyThreads = 256;
 
-// position -> element offset without layer and head, -1 where the slot has no page for it
-__device__ __forceinline__ long long place_of(const c2t_cache &c, int b, int held, long long position, int page_shift) {
+// the page that holds a position of slot b, -1 where it has none
+__device__ __forceinline__ int page_of(const c2t_cache &c, int b, int held, long long position, int page_shift) {
   const long long index = position >> page_shift;
   if (position < 0 || index >= held) return -1;
   const int page = c.table_dev[(long long)b * c.max_pages + index];
-  if (page < 0 || page >= c.n_pages) return -1;
+  return page < 0 || page >= c.n_pages ? -1 : page;
+}
+
+// the element offset of a position in that page, without layer and head
+__device__ __forceinline__ long long place_in(const c2t_cache &c, int page, long long position) {
   return page * c.page_stride + (position & (c.page_size - 1)) * c.token_stride;
 }
+
+// Does another slot hold the page?  Then nothing is written to it: a slot that was trimmed into a page which it shares with a fork would write over
+// that one's tokens.  (Asked of every position that is written: 64 sequences' 60 tokens take 6.8 us with and without it, their paths in 32 layers 16.0 and 15.5.)
+__device__ __forceinline__ bool is_shared(const c2t_cache &c, int page) { return c.refs_dev[page] > 1; }
 
 __device__ __forceinline__ int pages_for(const c2t_cache &c, int tokens) { return (tokens + c.page_size - 1) / c.page_size; }
 
@@ -283,12 +291,12 @@ __global__ void __launch_bounds__(kCopyThreads) append_kernel(c2t_cache c, int l
     const int j = (int)(i / per_token), r = (int)(i - (long long)j * per_token), h = r / vecs, vec = r - h * vecs;
     const long long from = b * in.seq_stride + j * in.token_stride + h * in.head_stride + vec * 8;
     const uint4 key = *reinterpret_cast<const uint4 *>(in.k + from), value = *reinterpret_cast<const uint4 *>(in.v + from);
-    const long long place = place_of(c, b, held, (long long)first + j, in.page_shift);
-    if (place < 0) {
+    const int page = page_of(c, b, held, (long long)first + j, in.page_shift);
+    if (page < 0 || is_shared(c, page)) {
       cache_fault(c, b, C2T_ST_BAD_PAGE);
       continue;
     }
-    const long long to = place + h * c.head_stride + vec * 8;
+    const long long to = place_in(c, page, (long long)first + j) + h * c.head_stride + vec * 8;
     *reinterpret_cast<uint4 *>(k + to) = key;
     *reinterpret_cast<uint4 *>(v + to) = value;
   }
@@ -310,9 +318,11 @@ __global__ void __launch_bounds__(kCopyThreads) compact_kernel(c2t_cache c, cons
   if (!faults && threadIdx.x < n) {
     const int d = threadIdx.x, held = held_pages(c, b);
     const int32_t *p = path + (long long)b * path_width;
-    from[d] = place_of(c, b, held, (long long)prefix + p[d], page_shift);
-    to[d] = place_of(c, b, held, (long long)prefix + d, page_shift);
-    if (from[d] < 0 || to[d] < 0 || p[d] < d || (d > 0 && p[d] <= p[d - 1])) atomicOr(&faults, 1);
+    const long long source = (long long)prefix + p[d], target = (long long)prefix + d;
+    const int from_page = page_of(c, b, held, source, page_shift), to_page = page_of(c, b, held, target, page_shift);
+    if (from_page < 0 || to_page < 0 || p[d] < d || (d > 0 && p[d] <= p[d - 1]) || (p[d] != d && is_shared(c, to_page))) atomicOr(&faults, 1);
+    from[d] = place_in(c, from_page, source);
+    to[d] = place_in(c, to_page, target);
   }
   __syncthreads();
   if (blockIdx.x == 0 && threadIdx.x == 0) {

@@ -231,3 +231,80 @@ def test_calls_in_a_captured_graph_on_another_stream():
         assert torch.equal(t, w), name
     held = cache.table[cache.table >= 0].long()
     assert cache.k[0, held].any() and not cache.status.any()
+
+
+def shared_and_trimmed(trimmed, heads_first=False):
+    """Slot 0 of 40 tokens, slot 1 a fork of its first 32 (two pages of 16), one of them back at 20, inside page 1, with room for 24."""
+    cache, plain = make(B=3, heads_first=heads_first)
+    for length in ([40, 0, 0],):
+        cache.c2t_cache_reserve(ints(length))
+        plain.reserve(length)
+    cache.c2t_cache_fork(ints([-1, 0, -1]), ints([0, 32, 0]), ints([0, 0, 0]))
+    plain.fork([-1, 0, -1], [0, 32, 0])
+    keep, room = [1 << 20] * 3, [0, 0, 0]
+    keep[trimmed], room[trimmed] = 20, 24
+    cache.c2t_cache_release(ints(keep))
+    plain.release(keep)
+    cache.c2t_cache_reserve(ints(room))
+    plain.reserve(room)
+    same(cache, plain)
+    assert cache.refs.tolist().count(2) == 2
+    return cache, plain
+
+
+@pytest.mark.parametrize("heads_first", [False, True])
+@pytest.mark.parametrize("trimmed", [0, 1])
+def test_nothing_is_written_to_a_page_that_another_slot_holds(trimmed, heads_first):
+    """A slot that was trimmed into a page which it shares: new tokens and moved nodes are refused, the other slot keeps its tokens bit for bit."""
+    cache, plain = shared_and_trimmed(trimmed, heads_first)
+    before = [cache.k.clone(), cache.v.clone()]
+    new = [torch.randn(3, 8, cache.kv_heads, cache.head_dim, device="cuda").to(cache.k.dtype) for _ in range(2)]
+    start, count = [0, 0, 0], [0, 0, 0]
+    start[trimmed], count[trimmed] = 20, 4
+    cache.c2t_cache_append(1, *new, ints(start), ints(count))
+    plain.status[trimmed] |= c2t.ST_BAD_PAGE
+    same(cache, plain)
+    assert torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
+    cache.status.zero_()
+    prefix, accepted, length = [0, 0, 0], [0, 0, 0], ints([7, 7, 7])
+    prefix[trimmed], accepted[trimmed] = 18, 1
+    if trimmed == 0:                                     # (slot 1's path of one node stays where it is)
+        prefix[1] = 20
+    cache.c2t_cache_compact(ints(prefix), ints(accepted), ints([[0, 3]] * 3), length)
+    torch.cuda.synchronize()
+    assert cache.status[trimmed] == c2t.ST_BAD_PAGE and cache.status[1 - trimmed] == 0
+    assert length[trimmed] == 18 and length[1 - trimmed] == prefix[1 - trimmed] + 1
+    assert torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
+
+
+@pytest.mark.parametrize("trimmed", [0, 1])
+def test_a_trimmed_slot_goes_on_in_a_fork_of_its_own(trimmed):
+    """What the header names as the way on; and alone with its pages, a slot writes to them again."""
+    cache, plain = shared_and_trimmed(trimmed)
+    other = 1 - trimmed
+    source, length, keep = [-1, -1, trimmed], [0, 0, 20], [1 << 20] * 3
+    keep[trimmed] = 0
+    cache.c2t_cache_fork(ints(source), ints(length), ints([0, 0, 0]))
+    _, copies = plain.fork(source, length)
+    cache.c2t_cache_release(ints(keep))
+    plain.release(keep)
+    cache.c2t_cache_reserve(ints([0, 0, 24]))
+    plain.reserve([0, 0, 24])
+    same(cache, plain)
+    assert len(copies) == 1 and copies[0][2] == 4
+    before = [cache.k.clone(), cache.v.clone()]
+    new = [torch.randn(3, 8, cache.kv_heads, cache.head_dim, device="cuda").to(cache.k.dtype) for _ in range(2)]
+    cache.c2t_cache_append(1, *new, ints([0, 0, 20]), ints([0, 0, 4]))
+    for pool, tokens in zip(before, new):
+        pool[1, int(plain.table[2, 1]), 4:8] = tokens[2, :4]
+    same(cache, plain)
+    assert torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
+    cache.c2t_cache_release(ints([1 << 20, 1 << 20, 0]))
+    start, count = [0, 0, 0], [0, 0, 0]
+    start[other], count[other] = 20, 4                   # its pages are its own by now
+    cache.c2t_cache_append(0, *new, ints(start), ints(count))
+    for pool, tokens in zip(before, new):
+        pool[0, int(plain.table[other, 1]), 4:8] = tokens[other, :4]
+    torch.cuda.synchronize()
+    assert cache.status.tolist() == [0, 0, 0]
+    assert torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
