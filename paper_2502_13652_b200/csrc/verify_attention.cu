@@ -1485,6 +1485,9 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   Params p;
   p.c = *cache;
   p.a = *attention;
+  // Without positions of their own no row is further than this from a key: such a window is none, and its differences stay within 32 bits.  (With
+  // positions only cached keys are compared with a row's own position, which is never before them.)
+  if (!p.a.position_ids_dev && p.a.window >= kMaxTokens + p.a.max_queries) p.a.window = 0;
   p.group = p.a.q_heads / p.c.kv_heads;
   const long long rows = (long long)p.a.max_queries * p.group, blocks = (rows + kBlockRows - 1) / kBlockRows;
   if (blocks * p.c.batch * p.c.kv_heads > 0x7FFFFFFF || rows * p.group > 0x7FFFFFFF) return C2T_ERANGE;

@@ -416,3 +416,14 @@ def test_two_streams_with_a_workspace_each():
     torch.cuda.synchronize()
     a.compare()
     b.compare()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 40, 2 ** 30 + 2 ** 24, 2 ** 30 + 100, 2 ** 30])
+@pytest.mark.parametrize("positions", [False, True])
+def test_windows_wider_than_any_cache_hide_nothing(window, positions):
+    """Nodes behind a row's own among them, which a mask may let it see: rows of 90 nodes, each of which sees all others."""
+    c = Case([100, 3, 0], [90, 40, 1], D=64, seed=2, window=window, sinks=1)
+    c.bits.fill_(-1)
+    if not positions:
+        c.positions = None
+    c.check()
