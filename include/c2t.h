@@ -78,7 +78,7 @@ typedef enum { C2T_ADD_FRONTIER = 0, C2T_ADD_ALL_SURVIVORS = 1 } c2t_tree_add;
 #define C2T_ST_ALL_NEGINF    4u
 #define C2T_ST_TREE_OVERFLOW 8u
 /* The library caught itself: a bounded wait inside the expand pass ran out (the row is given up and its
- * candidates dropped), or, in a build with -DC2T_DEBUG_BOUNDS, an index check failed (the access is skipped,
+ * candidates dropped), one inside c2t_verify_attention (every slot that the thread block had a share of gets the bit), or, in a build with -DC2T_DEBUG_BOUNDS, an index check failed (the access is skipped,
  * never made).  The results of the sequence in this step are unspecified; later steps are not affected.
  * Never set by data. */
 #define C2T_ST_INTERNAL      16u

@@ -118,6 +118,9 @@ struct Params {
   int grid;                                 // thread blocks of the main launch: G
   int join_step;                            // without a common factor with the other launch's
   int split;                                // 1: blocks of rows may be cut; 0: whole ones
+#ifdef C2T_DEBUG_BOUNDS
+  int tries;                                // of a wait
+#endif
   int least_tiles, more_tiles;              // of a piece, where all get equal ones, and how many more than an even deal they may have
   // Unfinished rows' sums over the values, two sets per thread block, and their maximum (scaled, base 2) and sum of weights.  Where a sequence has 32 rows at most
   // they lie side by side, the rows of a copy after those of the other, in a few megabytes: spread over places for 256 rows each, which is tens of megabytes, the
@@ -230,6 +233,9 @@ struct alignas(1024) Shared {
   Block block[kBlocks];
   uint32_t tmem;
   int gave_up;
+#ifdef C2T_DEBUG_BOUNDS
+  int tries;
+#endif
   uint32_t odd[8];
   long long warp_sum[kThreads / 32];
   int left, pair, head, k0, c0, c1, long_ones;
@@ -238,8 +244,17 @@ struct alignas(1024) Shared {
 constexpr int kMaxPairs = C2T_MAX_BATCH;    // for an even deal
 
 template <int D>
+__device__ __forceinline__ int tries_of(const Shared<D> &sh) {
+#ifdef C2T_DEBUG_BOUNDS
+  return sh.tries;
+#else
+  return kTries;
+#endif
+}
+
+template <int D>
 __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
-  for (int i = 0; i < kTries; ++i) {
+  for (int i = 0; i < tries_of(sh); ++i) {
     if (barrier_try(bar, parity)) return true;
     if ((i & 63) == 63 && *(volatile int *)&sh.gave_up) return false;
   }
@@ -251,12 +266,17 @@ __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t pari
 // ends on a vote, which all lanes are known to share: the tensor-memory instructions behind it must be reached by the whole warp at once.
 template <int D>
 __device__ __forceinline__ bool warp_wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
-  for (int i = 0; i < kTries; ++i) {
+  for (int i = 0; i < tries_of(sh); ++i) {
     if (__all_sync(~0u, barrier_try(bar, parity))) return true;
     if ((i & 63) == 63 && __any_sync(~0u, *(volatile int *)&sh.gave_up)) return false;
   }
   sh.gave_up = 1;
   return false;
+}
+
+// What is still on its way, to shared or tensor memory that is about to be let go.
+__device__ __forceinline__ void let_arrive(uint64_t *bar, uint32_t parity) {
+  for (int tries = 0; tries < kTries && !barrier_try(bar, parity); ++tries) {}
 }
 
 // A buffer of the ring and the parity of its barriers.  The copies' order: K_0 .. K_{ahead-1}, then V_t, K_{t+ahead} in turn.
@@ -595,6 +615,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     barrier_init(&sh.meet, kSoftmaxThreads);
     barrier_init_fence();
     sh.gave_up = 0;
+#ifdef C2T_DEBUG_BOUNDS
+    sh.tries = p.tries;
+#endif
     sh.left = sh.pair = sh.head = sh.k0 = 0;
     sh.c0 = -1;
     sh.long_ones = 0;
@@ -705,7 +728,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     const Block &w = sh.block[i % kBlocks];
     if (w.rows != 0 && (w.b < 0 || w.b >= p.c.batch || w.head < 0 || w.head >= p.c.kv_heads || w.row0 < 0 || w.rows < 0 || w.rows > kBlockRows || w.k0 < 0 ||
                         w.k1 <= w.k0 || w.k1 > w.tiles || w.n > p.a.max_queries || w.row0 + w.rows > w.n * p.group)) {
-      if (p.c.status_dev) atomicOr(p.c.status_dev, C2T_ST_INTERNAL);
       sh.gave_up = 1;
       return false;
     }
@@ -762,8 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           }
         }
       }
-      if (copied > 0 && *(volatile int *)&sh.gave_up)           // nothing may arrive in a block's memory that has ended
-        for (int tries = 0; tries < kTries && !barrier_try(&sh.queries, (copied - 1) & 1); ++tries) {}
+      if (copied > 0) let_arrive(&sh.queries, (copied - 1) & 1);                // (nothing may arrive in a block's memory that has ended, whoever gave up)
     }
     __syncwarp();
   } else if (warp == 9) {
@@ -813,14 +834,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         ++filled;
         page = next; values = next_values; key = next_key;
       }
-      if (!ok) {
-        if (lane == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
-        break;
-      }
+      if (!ok) break;
     }
-    if (!ok && lane == 0)                   // nothing may arrive in a block's memory that has ended
-      for (int i = max(filled - kRing, 0); i < filled; ++i)
-        for (int tries = 0; tries < kTries && !barrier_try(sh.full + i % kRing, i / kRing & 1); ++tries) {}
+    if (lane == 0)                          // (nor here)
+      for (int i = max(filled - kRing, 0); i < filled; ++i) let_arrive(sh.full + i % kRing, i / kRing & 1);
     __syncwarp();
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
@@ -929,9 +946,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
       __syncwarp();
       keys = vals;
     }
-    if (!ok && leader) {                    // what is in flight must not outlive its tensor memory
-      products_commit(&sh.done);
-      for (int tries = 0; tries < kTries && !barrier_try(&sh.done, item & 1); ++tries) {}
+    if (leader) {                           // what is in flight must not outlive its tensor memory
+      if (!ok) products_commit(&sh.done);
+      if (!ok || item > 0) let_arrive(&sh.done, (ok ? item - 1 : item) & 1);
     }
     __syncwarp();
   } else {
@@ -1012,10 +1029,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
           barrier_arrive(sh.weights + s);
         }
       }
-      if (!ok || !(ok = warp_wait(sh, &sh.done, item & 1))) {
-        if (tid == 0) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
-        break;
-      }
+      if (!ok || !(ok = warp_wait(sh, &sh.done, item & 1))) break;
       tmem_fence_after();
 
       // ---- what the thread block has of its rows: finished, or a part for the other launch to add up
@@ -1162,6 +1176,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
   tmem_fence_before();
   __syncthreads();
   if (warp == 8) tmem_free(tmem, kMathColumns);
+  if (sh.gave_up) {                         // the rows of every slot of the share are in doubt
+    if (!p.split) {
+      for (int pair = tid; pair < n_pairs; pair += kThreads) {
+        const Block w = block_of(p, pair);
+        const int before = (int)((long long)pair * p.c.kv_heads % G), turn = (int)blockIdx.x - before + ((int)blockIdx.x < before ? G : 0);
+        if (w.tiles > 0 && turn < p.c.kv_heads) cache_fault(p.c, w.b, C2T_ST_INTERNAL);
+      }
+    } else if (tid == 0) {
+      int left = sh.left, first = sh.pair;
+      for (int pair = first; pair < n_pairs && left > 0; ++pair) {
+        const Block w = block_of(p, pair);
+        if (w.tiles == 0) continue;
+        cache_fault(p.c, w.b, C2T_ST_INTERNAL);
+        left -= w.tiles * p.c.kv_heads - (pair == first ? sh.head * w.tiles + sh.k0 : 0);
+      }
+    }
+  }
 }
 
 // ---------------------------------------------------------------- parts of rows that several thread blocks read the keys of
@@ -1470,6 +1501,10 @@ using namespace c2t;
 
 extern "C" {
 
+#ifdef C2T_DEBUG_BOUNDS
+int c2t_debug_attention_wait_limit = kTries;                    // tests let the waits run out
+#endif
+
 size_t c2t_verify_attention_workspace_bytes(const c2t_cache *cache, int32_t q_heads, int32_t max_queries) {
   if (check_cache(cache) != C2T_OK || q_heads < 1 || q_heads % cache->kv_heads || max_queries < 1) return 0;
   return workspace_of(*cache).bytes;
@@ -1499,6 +1534,9 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   // Equal pieces against an even deal: 8 trees of 60 nodes, 32 heads, behind 2048 tokens take 38.8 us and 41.2, a token of 32
   // heads behind 6000 others 17.0 and 20.5.  A piece of fewer tiles than these costs more to join than it saves: 8 such trees behind 300 take 23.7 us with pieces of 2 tiles, 20.2 of 3.
   p.least_tiles = rows > kRows ? 3 : 2;
+#ifdef C2T_DEBUG_BOUNDS
+  p.tries = c2t_debug_attention_wait_limit;
+#endif
   p.more_tiles = rows > kRows ? 3 : 4;
   char *base = static_cast<char *>(workspace_dev);
   p.part_o = reinterpret_cast<float *>(base + at.o);
