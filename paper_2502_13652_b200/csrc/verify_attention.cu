@@ -60,38 +60,67 @@ template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
 
-// One warp, one row (b, i, h): the keys in [lo, hi) one after the other, with the running maximum m (in units of the exponent, base 2), the sum l of
-// the weights and their sum over the values, D / 32 elements a lane.
+// One warp, one row (b, i, h): the keys in [lo, hi) in order, with the running maximum m (in units of the exponent, base 2), the sum l of
+// the weights and their sum over the values, D / 32 elements a lane.  The loads of kAtOnce keys go out together.
 template <typename T, int D>
 __device__ void attend_row(const c2t_cache &c, const c2t_attention &a, const Sight &see, int b, int i, int h, int lo, int hi, float &m, float &l,
                            float *o) {
-  constexpr int E = D / 32;
+  constexpr int E = D / 32, kAtOnce = D == 128 ? 8 : 2;         // (with more the kernel that calls this spills registers)
+  using Elements = typename std::conditional<E == 4, uint2, uint32_t>::type;      // of a lane
   const int lane = threadIdx.x & 31;
   const T *q = static_cast<const T *>(a.q_dev) + b * a.q_seq_stride + i * a.q_token_stride + h * a.q_head_stride + lane * E;
   float qe[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) qe[e] = to_float(q[e]);
   const long long head = a.layer * c.layer_stride + (h / (a.q_heads / c.kv_heads)) * c.head_stride + lane * E;
-  const int own = see.position(i);
+  const int own = see.position(i), page_shift = __ffs(c.page_size) - 1;
   const float unit = a.scale * kLog2e;
-  for (int p = lo; p < hi; ++p) {
-    if (!see.sees(i, own, p)) continue;
-    const int page = c.table_dev[(long long)b * c.max_pages + p / c.page_size];
-    if (page < 0 || page >= c.n_pages) {
-      cache_fault(c, b, C2T_ST_BAD_PAGE);
-      continue;
+#pragma unroll 1
+  for (int p = lo; p < hi; p += kAtOnce) {
+    bool seen[kAtOnce];
+    long long at[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      seen[u] = p + u < hi && see.sees(i, own, p + u);
+      const int page = seen[u] ? c.table_dev[(long long)b * c.max_pages + ((p + u) >> page_shift)] : 0;
+      const bool there = page >= 0 && page < c.n_pages;
+      if (!there) cache_fault(c, b, C2T_ST_BAD_PAGE);
+      seen[u] &= there;
+      at[u] = head + (there ? page : 0) * c.page_stride + ((p + u) & (c.page_size - 1)) * c.token_stride;       // (some place of the pool)
     }
-    const long long at = head + page * c.page_stride + (p & (c.page_size - 1)) * c.token_stride;
-    const T *k = static_cast<const T *>(c.k_dev) + at, *v = static_cast<const T *>(c.v_dev) + at;
-    float s = 0.f;
+    Elements x[kAtOnce];                    // of the keys, then of the values
+    auto load = [&](const void *pool) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += qe[e] * to_float(k[e]);
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-    s *= unit;
-    const float top = fmaxf(m, s), keep = m == top ? 1.f : exp2f(m - top), w = s == -INFINITY ? 0.f : exp2f(s - top);
-    l = l * keep + w;
+      for (int u = 0; u < kAtOnce; ++u) x[u] = *reinterpret_cast<const Elements *>(static_cast<const T *>(pool) + at[u]);
+    };
+    float s[kAtOnce], top = m;
+    load(c.k_dev);
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * keep + w * to_float(v[e]);
+    for (int u = 0; u < kAtOnce; ++u) {
+      s[u] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[u] += qe[e] * to_float(reinterpret_cast<const T *>(&x[u])[e]);
+    }
+    load(c.v_dev);
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) s[u] += __shfl_xor_sync(~0u, s[u], d);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      s[u] = seen[u] ? s[u] * unit : -INFINITY;
+      top = fmaxf(top, s[u]);
+    }
+    const float keep = m == top ? 1.f : exp2f(m - top);
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= keep;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const float w = s[u] == -INFINITY ? 0.f : exp2f(s[u] - top);
+      l += w;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += seen[u] ? w * to_float(reinterpret_cast<const T *>(&x[u])[e]) : 0.f;
+    }
     m = top;
   }
 }
@@ -211,7 +240,7 @@ template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 
 // Of 16 powers of two, 2 kProducts are products and sums instead of the special-function unit's.  64 sequences' tokens behind 4096: 136 us with 1, 139 with 0, 136 with 2;
 // trees of 8 x 2048 38.8, 39.6, 38.9; of 1 x 16000 53.4, 52.6, 53.7; a chunk of 2 x 2048 behind 6000 452, 452, 461.
 constexpr int kProducts = 1;
-constexpr int kTries = 1 << 20;             // of a wait, 3900 cycles each: after two seconds the block gives up
+constexpr int kTries = 1 << 20;             // of a wait, 3900 cycles each: after two seconds the block gives up (but see goes_on)
 
 template <int D> __device__ __forceinline__ constexpr int weights_at(int s) { return D == 64 ? 384 + s * 64 : s * kTile; }
 
@@ -233,6 +262,8 @@ struct alignas(1024) Shared {
   Block block[kBlocks];
   uint32_t tmem;
   int gave_up;
+  int redoing;                              // warps that do rows once more
+  uint32_t redo_ended;                      // when the last one was through; 0: none so far
 #ifdef C2T_DEBUG_BOUNDS
   int tries;
 #endif
@@ -252,9 +283,25 @@ __device__ __forceinline__ int tries_of(const Shared<D> &sh) {
 #endif
 }
 
+__device__ __forceinline__ uint32_t milliseconds() {            // of 2^20 ns; never 0
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return (uint32_t)(t >> 20) | 1;
+}
+
+// A wait has had its tries: it goes on while a warp does rows once more, which takes as long as their keys are many, and for two seconds behind that.  (Asked
+// only then: with the question in a wait's loop a chunk of 2 x 2048 tokens behind 6000 took 531 us instead of 517.)
+template <int D>
+__device__ __noinline__ bool goes_on(Shared<D> &sh) {
+  if (tries_of(sh) != kTries) return false;
+  if (*(volatile int *)&sh.redoing > 0) return true;
+  const uint32_t ended = *(volatile uint32_t *)&sh.redo_ended;                  // (written before the last one stops counting)
+  return ended != 0 && milliseconds() - ended < 2000;
+}
+
 template <int D>
 __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
-  for (int i = 0; i < tries_of(sh); ++i) {
+  for (int i = 0; i < tries_of(sh) || goes_on(sh); ++i) {
     if (barrier_try(bar, parity)) return true;
     if ((i & 63) == 63 && *(volatile int *)&sh.gave_up) return false;
   }
@@ -266,7 +313,7 @@ __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t pari
 // ends on a vote, which all lanes are known to share: the tensor-memory instructions behind it must be reached by the whole warp at once.
 template <int D>
 __device__ __forceinline__ bool warp_wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
-  for (int i = 0; i < tries_of(sh); ++i) {
+  for (int i = 0; i < tries_of(sh) || __any_sync(~0u, goes_on(sh)); ++i) {
     if (__all_sync(~0u, barrier_try(bar, parity))) return true;
     if ((i & 63) == 63 && __any_sync(~0u, *(volatile int *)&sh.gave_up)) return false;
   }
@@ -614,7 +661,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     barrier_init(&sh.queries_free, kSoftmaxThreads);
     barrier_init(&sh.meet, kSoftmaxThreads);
     barrier_init_fence();
-    sh.gave_up = 0;
+    sh.gave_up = sh.redoing = 0;
+    sh.redo_ended = 0;
 #ifdef C2T_DEBUG_BOUNDS
     sh.tries = p.tries;
 #endif
@@ -1147,7 +1195,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         }
         __syncwarp();
       }
-      fine |= !live;
+      fine |= !live || l != l;              // (a row whose sum of weights is none stays so: a logit that it sees is none)
       if (whole && !own_rows) {
         const uint32_t odd = __ballot_sync(~0u, !fine);
         if (lane == 0) sh.odd[warp] = odd;
@@ -1159,11 +1207,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
         for (int a = r0 + lane; a < kRows && lane < rows_here; a += copy_rows) fine &= !(sh.odd[s * 4 + (a >> 5)] >> (a & 31) & 1);
         fine |= r0 + lane >= w.rows;
       }
-      for (uint32_t again = __ballot_sync(~0u, !fine); again; again &= again - 1) {
+      const uint32_t odd_rows = __ballot_sync(~0u, !fine);
+      if (odd_rows != 0 && lane == 0) atomicAdd(&sh.redoing, 1);
+      for (uint32_t again = odd_rows; again; again &= again - 1) {
         // (a lane stands for its own row of the block, or, where there were copies to add up, for one of the rows that the warp wrote)
         const int from_lane = __ffs(again) - 1, r = __shfl_sync(~0u, whole && !own_rows ? r0 + lane : my_row, from_lane), at = __shfl_sync(~0u, place, from_lane);
         once_more<T, D>(p, w, r, whole ? 0 : first_column, whole ? kTile : copy_rows, column0, columns, whole, __shfl_sync(~0u, m, from_lane),
                         p.part_o + (part * (D / 4) * p.part_rows + at) * 4);
+      }
+      if (odd_rows != 0 && lane == 0) {
+        *(volatile uint32_t *)&sh.redo_ended = milliseconds();
+        __threadfence_block();
+        atomicAdd(&sh.redoing, -1);
       }
       if (p.copy_queries) {
         shared_writes_fence();

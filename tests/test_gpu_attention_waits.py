@@ -1,9 +1,16 @@
-"""The attention's bounded waits: where one runs out the slots that it concerns are reported."""
+"""The attention's bounded waits: they outlast rows that are done once more, key by key, and where one runs out the slots that it
+concerns are reported."""
+import math
 import os
 import subprocess
 import sys
 
 import pytest
+import torch
+
+import paper_2502_13652_b200 as c2t
+from plain_forms import half_step
+from test_gpu_attention import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -14,6 +21,70 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 def _built():
     from paper_2502_13652_b200 import build
     build.build()
+
+
+def repeated(c, b, h, times, tokens):
+    """Rows of slot b and head h in 64 bits, over keys that are there `times` often: out, lse and the tolerances of plain_forms.attend."""
+    N, D, dtype = c.Nq, c.D, c.dtype
+    kk, vv = (pool[0].reshape(-1, c.G, c.D)[tokens, h].double() for pool in (c.k, c.v))
+    see = torch.ones(N, len(tokens), dtype=torch.bool)
+    see[:, -N:] = ((c.bits[b][:, torch.arange(N) // 64] >> (torch.arange(N) % 64)) & 1).bool()
+    q, scale, u = c.q[b, :, h].double(), D ** -0.5, half_step(dtype)
+    x = (q @ kk.T * scale).masked_fill(~see, -math.inf)
+    top = x.amax(1, keepdim=True)
+    w = torch.exp(x - top) * times
+    total = w.sum(1, keepdim=True)
+    w /= total
+    out, lse = w @ vv, (top + total.log())[:, 0]
+    away = torch.where(see, scale * D * 2.0 ** -23 * (q.abs() @ kk.abs().T) + 2.0 ** -22 * (q @ kk.T * scale).abs(), 0.0).amax(1)
+    return out, lse, u * out.abs() + (u + float(times.sum()) * 2.0 ** -23 + 2.0 ** -18 + 2.1 * away[:, None]) * (w @ vv.abs()), away + 2.0 ** -18
+
+
+@pytest.mark.parametrize("D,dtype", [(64, torch.bfloat16), (128, torch.float16)])
+def test_rows_done_once_more_behind_a_long_prefix(D, dtype):
+    """A node that only its own row sees holds a NaN: all other rows of two heads are done once more over 350000 keys, in 4 or 5 seconds, longer than any wait
+    lasts otherwise.  The heads and the slot whose tiles the same thread blocks take behind those rows are right, and so are the rows themselves."""
+    heads, N, page, prefix = torch.cuda.get_device_properties(0).multi_processor_count, 256, 256, 350000
+    c = Case([512, 40], [N, N], H=heads, G=heads, D=D, page=page, dtype=dtype, seed=D)
+    c.prefix[0] = prefix                                 # the two pages of the prefix over and over
+    tail, rest = divmod(prefix, page)
+    table = torch.full((2, tail + 2), -1, dtype=torch.int32)
+    assert rest + N <= 2 * page
+    table[0, :tail] = c.table[0, torch.arange(tail) % 2]
+    table[0, tail] = c.table[0, 2]
+    table[0, tail + 1] = [p for p in range(c.k.shape[1]) if p not in set(c.table[c.table >= 0].tolist())][0]
+    table[1, :2] = c.table[1, :2]
+    c.table, c.held = table, torch.tensor([tail + 2, 2], dtype=torch.int32)
+    c.bits[:, :, 0] &= ~(1 << 9)
+    c.bits[:, 9, 0] |= 1 << 9
+    c.positions = None
+    bad = [0, heads - 1]                                 # the first thread block's first head, the last one's last
+    place = int(table[0, (prefix + 9) // page]), (prefix + 9) % page
+    clean = c.v[0, place[0], place[1]].clone()
+    c.v[0, place[0], place[1], bad] = math.nan
+    c.on_device()
+    c.call()
+    torch.cuda.synchronize()
+    assert c.cache.status.tolist() == [0, 0]
+    c.v[0, place[0], place[1]] = clean
+    got, got_lse = c.out.cpu().double(), c.lse.cpu().double()
+    for b in range(2):
+        end = prefix if b == 0 else 40
+        at = torch.arange(prefix - rest if b == 0 else 0, end + N)
+        tokens, times = table[b, at // page].long() * page + at % page, torch.ones(len(at), dtype=torch.float64)
+        if b == 0:
+            again = torch.cat([int(table[0, j]) * page + torch.arange(page) for j in range(2)])
+            tokens = torch.cat([again, tokens])
+            times = torch.cat([torch.full((page,), float((tail + 1) // 2)), torch.full((page,), float(tail // 2)), times.float()]).double()
+            assert float(times.sum()) == prefix + N
+        for h in range(heads):
+            out, lse, tol, tol_lse = repeated(c, b, h, times, tokens)
+            row = torch.ones(N, dtype=torch.bool)
+            if b == 0 and h in bad:
+                row[9] = False
+                assert bool(torch.isnan(got[0, 9, h]).all())
+            assert bool(((got[b, :, h] - out).abs() <= tol)[row].all()), (b, h)
+            assert bool(((got_lse[b, :, h] - lse).abs() <= tol_lse)[row].all()), (b, h)
 
 
 GIVE_UP = r"""
