@@ -577,7 +577,8 @@ int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, con
  * n_queries is cut to max_queries; positions without a held page are not seen (C2T_ST_BAD_PAGE).  A page number out of range among the
  * held ones sets that bit too and leaves the slot's rows unspecified, but nothing out of bounds is touched.
  * A prefix_len below 0 counts as 0.
- * Products are of 16 bits with 32-bit sums; the weights are rounded to the cache's type for the second product.  Two launches at most.
+ * Products are of 16 bits with 32-bit sums; the weights are rounded to the cache's type for the second product (f16: or to a multiple of 2^-30 of the row's
+ * largest weight, whichever is coarser).  Two launches at most.
  */
 typedef struct {
   int32_t layer;

@@ -170,7 +170,12 @@ struct Block {                              // with the tiles [k0, k1) of it tha
   int b, head, row0, rows;                  // key head; first row; rows that are there (0: no block)
   int prefix, n, keys;                      // of the sequence, as in Sight
   int sink_tiles, first_tile, tiles, k0, k1;
-  __device__ __forceinline__ int key0(int t) const { return (t < sink_tiles ? t : first_tile + t - sink_tiles) * kTile; }
+  // Long blocks begin with the second tile, go on to the last, and end with the first and the sinks': of those a row with a window may see a few keys only,
+  // and its maximum would have to be raised behind them.  (In ascending order 16 windows of 1024, 64 heads of 64, take 96 us instead of 76.)
+  __device__ __forceinline__ int key0(int t) const {
+    const int near = tiles - sink_tiles;
+    return (t >= near ? t - near : near <= 2 ? first_tile + t : first_tile + (t + 1 < near ? t + 1 : 0)) * kTile;
+  }
 };
 
 __device__ __forceinline__ Block block_of(const Params &p, int pair) {
@@ -228,15 +233,17 @@ struct Deal {
 //   warp 8    issues the products: logits S = Q K^T (both from shared memory), and O += P V with P, the weights, in tensor memory in S's place
 //   warp 9    copies the tiles of keys and values, a box per page and 64 elements of a head, into a ring of buffers
 //   warp 10   walks through the thread block's share and describes the next blocks of rows to the others
-// The running maximum is only raised when a row's new one is more than 2^14 (bf16: 2^40) in weight above it: then O and the sum are rescaled.  Weights are
-// so at most 2^14, which f16 holds, or 2^40, of which 32 bits hold any sum; a weight's precision does not depend on its size.  (At 2^8 rows that
-// begin with a few first keys asked for a second pass in their second tile: 16 windows of 1024, 64 heads, 82 -> 102 us.)
+// The running maximum m is only raised when a row's new one is more than 2^9 (bf16: 2^40) in weight above it: then O and the sum are rescaled.  A weight is
+// 2^kLift at m, so at most 2^15, which f16 holds, or 2^40, of which 32 bits hold any sum.  Of f16, whose numbers end at 2^-24, the lift keeps the weights of
+// long flat tails: a weight is off by half a step or 2^-31 of the largest, whichever is more, so that 2^20 keys add up to half a step (without it 2^14 keys).
+// Every further bit of it asks more rows for a second pass: 16 windows of 1024, 64 heads of 64, take 75.5 us with 0, 4, 5 and 6, 78 with 8.
 // Up to 32 (64) rows lie in the accumulator four times (twice), and each copy takes a quarter (half) of a tile's keys, with weights of 0
 // for the others: all warps have work then, and a tile's softmax, which is what such a block waits for, a quarter of the steps.
 
 constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x D; P in the place of S, with heads of 64 in columns of its own
-template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 14.f : 40.f;
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 6.f : 0.f;
+template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 15.f - kLift<T> : 40.f;
 // Of 16 powers of two, 2 kProducts are products and sums instead of the special-function unit's.  64 sequences' tokens behind 4096: 136 us with 1, 139 with 0, 136 with 2;
 // trees of 8 x 2048 38.8, 39.6, 38.9; of 1 x 16000 53.4, 52.6, 53.7; a chunk of 2 x 2048 behind 6000 452, 452, 461.
 constexpr int kProducts = 1;
@@ -512,7 +519,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t my_s, uint32_t my_w, uint3
         }
       }
     }
-    const float shift = m == -INFINITY ? 0.f : -m * unit;
+    const float shift = m == -INFINITY ? 0.f : kLift<T> - m * unit;
     float top[2] = {-INFINITY, -INFINITY};
     sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
     __syncwarp();
@@ -1082,7 +1089,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
 
       // ---- what the thread block has of its rows: finished, or a part for the other launch to add up
       const bool whole = w.k0 == 0 && w.k1 == w.tiles;
-      m = m == -INFINITY ? m : m * unit;
+      m = m == -INFINITY ? m : m * unit - kLift<T>;          // (of which the weights are the powers' differences)
       float factor0 = 1.f, factor1 = 0.f;
       if (!two) {                           // over the two accumulators and, for a finished row, its copies
         sh.ml[s][row] = make_float2(m, l);

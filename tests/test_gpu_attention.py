@@ -427,3 +427,28 @@ def test_windows_wider_than_any_cache_hide_nothing(window, positions):
     if not positions:
         c.positions = None
     c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N", [1, 140])
+@pytest.mark.parametrize("first", [0, 200, 9000])
+def test_a_long_flat_tail_behind_one_large_weight_in_f16(D, N, first):
+    """16384 keys whose weights are 2^-25.25 of one key's each: less than half of f16's smallest number, 4e-4 of the row together, and all of it where the
+    one key's value is 0.  Beside the usual tolerance each weight may be off by 2^-31 of the largest (half of 2^-30).  The same keys for more sequences
+    than there are thread blocks, so that few rows are cut into parts, which have maxima of their own."""
+    c = Case([16384], [N], D=D, H=1, G=1, page=64, dtype=torch.float16, is_tree=False, scale=1.0)
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.k[..., 0] = -17.5
+    c.v.fill_(1.0)
+    page, at = int(c.table[0, first // 64]), first % 64
+    c.k[0, page, at, :, 0], c.v[0, page, at] = 0.0, 0.0
+    out, lse, tol, tol_lse = c.want()
+    assert 3e-4 < float(out[0, 0, 0, 0]) < 5e-4
+    tol += (16384 + N) * 2.0 ** -31
+    c.B = 160
+    c.q, c.table, c.held, c.n, c.prefix, out, lse, tol, tol_lse = (torch.cat([t] * c.B) for t in (c.q, c.table, c.held, c.n, c.prefix, out, lse, tol, tol_lse))
+    c.on_device()
+    c.call()
+    torch.cuda.synchronize()
+    c.compare(want=(out, lse, tol, tol_lse))
