@@ -15,6 +15,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int kMaxTokens = 0x40000000;      // of a slot; with the queries' number 32 bits hold every position
+constexpr int kAnyKey = 0x60000000;         // behind every key of a slot
 
 // What the rows of a sequence see.
 struct Sight {
@@ -363,7 +364,8 @@ __device__ __forceinline__ bool is_woven(const Params &p, int rows) { return p.f
 // bits 0..31: columns c < n
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
-// which of the 32 keys from `key` row i sees
+// Which of the 32 keys from `key` row i sees.  (key may be below 0 where a last box reaches to the left of the first key; windows, sinks and positions may be
+// any numbers: bounds are brought among the keys before they are compared, so that nothing passes 32 bits.)
 __device__ __forceinline__ uint32_t sight_bits(const Sight &s, int i, int own, int key) {
   uint32_t on = low_bits(s.keys - key);
   const int node = key - s.prefix;          // of the first of them
@@ -381,8 +383,8 @@ __device__ __forceinline__ uint32_t sight_bits(const Sight &s, int i, int own, i
     }
   }
   if (s.window > 0) {
-    const uint32_t sink = low_bits(s.sinks - key);
-    uint32_t near = ~low_bits(own - s.window + 1 - key);
+    const uint32_t sink = low_bits(min(s.sinks, kAnyKey) - key);
+    uint32_t near = ~low_bits(min(max(own - s.window + 1, 0), kAnyKey) - key);
     if (node + 31 >= 0 && s.positions && own - s.prefix >= s.window) {          // nodes' positions are their levels': one by one
       uint32_t nodes = tree & ~cached & on;
       tree &= ~nodes;
@@ -1582,9 +1584,6 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   Params p;
   p.c = *cache;
   p.a = *attention;
-  // Without positions of their own no row is further than this from a key: such a window is none, and its differences stay within 32 bits.  (With
-  // positions only cached keys are compared with a row's own position, which is never before them.)
-  if (!p.a.position_ids_dev && p.a.window >= kMaxTokens + p.a.max_queries) p.a.window = 0;
   p.group = p.a.q_heads / p.c.kv_heads;
   const long long rows = (long long)p.a.max_queries * p.group, blocks = (rows + kBlockRows - 1) / kBlockRows;
   if (blocks * p.c.batch * p.c.kv_heads > 0x7FFFFFFF || rows * p.group > 0x7FFFFFFF) return C2T_ERANGE;

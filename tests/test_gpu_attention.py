@@ -452,3 +452,15 @@ def test_a_long_flat_tail_behind_one_large_weight_in_f16(D, N, first):
     c.call()
     torch.cuda.synchronize()
     c.compare(want=(out, lse, tol, tol_lse))
+
+
+@pytest.mark.parametrize("page", [8, 256])
+@pytest.mark.parametrize("window,sinks,up", [(1, 2 ** 31 - 1, 0), (40, 2 ** 31 - 1, 0), (40, 2 ** 31 - 100, 7), (1, 3, 2 ** 31 - 800), (2 ** 31 - 1, 0, 2 ** 31 - 800),
+                                             (2 ** 31 - 700, 3, 2 ** 31 - 800), (5, 2 ** 31 - 1, 2 ** 31 - 800), (5, 2 ** 31 - 760, 2 ** 31 - 800)])
+def test_windows_sinks_and_positions_near_32_bits(window, sinks, up, page):
+    """Positions `up` behind the usual ones; sequences shorter than a page, whose last box reaches to the left of their first key."""
+    c = Case([60, 3, 0, 700, 130], [1, 20, 33, 60, 60], D=64, H=4, G=2, page=page, window=window, sinks=sinks, seed=7)
+    c.positions = (c.prefix[:, None] + torch.minimum(c.positions - c.prefix[:, None], torch.tensor(9)) + min(up, 2 ** 31 - 1 - 710)).to(torch.int32)
+    c.check()
+    c.positions = None
+    c.check()
