@@ -571,7 +571,8 @@ int c2t_cache_compact(const c2t_cache *cache, const int32_t *prefix_len_dev, con
  * window > 0 keeps of these the positions less than `window` before the query's own, and the first `sinks` positions, which stay visible.
  * A node's own position is position_ids[b, i] (c2t_build_verify's; NULL: prefix_len + i; a value below prefix_len[b] counts as
  * prefix_len[b]).  A row that sees nothing gets zeros and lse = -inf.  Keys and values that no mask lets a row see do not reach it,
- * whatever they hold (NaN and infinities included).
+ * whatever they hold (NaN and infinities included; but rows that were multiplied with such a value are then computed once more, key by key, at 0.3 to 0.4 us a
+ * key and row of a warp's).
  * Query head h reads key head h / (q_heads / kv_heads).  Rows i >= n_queries[b] of out and lse are not written; what they hold in q does not
  * matter.  out must not overlap q.  Strides of q may be 0, those of out that are stepped over may not.
  * n_queries is cut to max_queries; positions without a held page are not seen (C2T_ST_BAD_PAGE).  A page number out of range among the

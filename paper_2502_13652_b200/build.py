@@ -21,8 +21,8 @@ def _newest_source() -> float:
 
 
 def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False) -> str:
-    """Compiles the library if it is older than its sources.  debug_bounds: the variant whose kernels check the
-    indices of their own writes and report a failed check in a status bit (C2T_ST_INTERNAL)."""
+    """Compiles the library if it is older than its sources.  debug_bounds: the variant whose kernels of the levels, the tree and the
+    walk check the indices of their own writes and report a failed check in a status bit (C2T_ST_INTERNAL), and whose waits' limits tests can set."""
     lib = LIB_DEBUG if debug_bounds else LIB
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= _newest_source():
         return lib

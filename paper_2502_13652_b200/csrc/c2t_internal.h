@@ -33,8 +33,8 @@ __device__ __forceinline__ int32_t key_token(unsigned long long k) {
 constexpr float kNegInfAsFinite = -1.7e38f;   // anything at or below this was -inf (or as good as)
 
 // ---------------------------------------------------------------- index checks
-// A build with -DC2T_DEBUG_BOUNDS checks the indices of the kernels' writes to shared memory queues, pools and
-// workspace records: a failed check sets C2T_ST_INTERNAL in the given status word (if there is one) and the guarded
+// A build with -DC2T_DEBUG_BOUNDS checks the indices of the writes to shared memory queues, pools and workspace records in the kernels of
+// the levels, the tree and the walk (of the calls without a context it checks what an attention's blocks of rows are described as): a failed check sets C2T_ST_INTERNAL in the given status word (if there is one) and the guarded
 // access is skipped.  It stands in for a memory checker where none can be run.  In a normal build the check is the
 // constant `true`.
 #ifdef __CUDACC__

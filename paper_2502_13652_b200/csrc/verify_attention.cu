@@ -1,4 +1,8 @@
 // Attention of a tree's nodes, a prompt's chunk or single tokens over the paged cache.  See include/c2t.h.
+//
+// Times in this file: one call among others, its inputs new from call to call; trees of 60 nodes; unless said otherwise 32 heads of 128, 8 key heads, bf16, pages
+// of 16.  "A window" is trees of 16 sequences behind 20000 with a window of 1024 and 4 sinks, 64 heads of 64 over 8 key heads, f16, pages of 32; "a chunk" is
+// 2 x 2048 tokens behind 6000.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -172,7 +176,7 @@ struct Block {                              // with the tiles [k0, k1) of it tha
   int prefix, n, keys;                      // of the sequence, as in Sight
   int sink_tiles, first_tile, tiles, k0, k1;
   // Long blocks begin with the second tile, go on to the last, and end with the first and the sinks': of those a row with a window may see a few keys only,
-  // and its maximum would have to be raised behind them.  (In ascending order 16 windows of 1024, 64 heads of 64, take 96 us instead of 76.)
+  // and its maximum would have to be raised behind them.  (With the sinks first and the others in ascending order a window takes 95 us, with the sinks last 90, so 76.)
   __device__ __forceinline__ int key0(int t) const {
     const int near = tiles - sink_tiles;
     return (t >= near ? t - near : near <= 2 ? first_tile + t : first_tile + (t + 1 < near ? t + 1 : 0)) * kTile;
@@ -237,7 +241,7 @@ struct Deal {
 // The running maximum m is only raised when a row's new one is more than 2^9 (bf16: 2^40) in weight above it: then O and the sum are rescaled.  A weight is
 // 2^kLift at m, so at most 2^15, which f16 holds, or 2^40, of which 32 bits hold any sum.  Of f16, whose numbers end at 2^-24, the lift keeps the weights of
 // long flat tails: a weight is off by half a step or 2^-31 of the largest, whichever is more, so that 2^20 keys add up to half a step (without it 2^14 keys).
-// Every further bit of it asks more rows for a second pass: 16 windows of 1024, 64 heads of 64, take 75.5 us with 0, 4, 5 and 6, 78 with 8.
+// Every further bit of it asks more rows for a second pass: a window takes 74.5 us with 0, 75.7 with 6, 78 with 8.
 // Up to 32 (64) rows lie in the accumulator four times (twice), and each copy takes a quarter (half) of a tile's keys, with weights of 0
 // for the others: all warps have work then, and a tile's softmax, which is what such a block waits for, a quarter of the steps.
 
@@ -245,8 +249,8 @@ constexpr int kSoftmaxThreads = 256, kThreads = 352;
 constexpr int kMathColumns = 512;           // of tensor memory: S 2 x 128, O 2 x D; P in the place of S, with heads of 64 in columns of its own
 template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 6.f : 0.f;
 template <typename T> constexpr float kRaise = std::is_same<T, __half>::value ? 15.f - kLift<T> : 40.f;
-// Of 16 powers of two, 2 kProducts are products and sums instead of the special-function unit's.  64 sequences' tokens behind 4096: 136 us with 1, 139 with 0, 136 with 2;
-// trees of 8 x 2048 38.8, 39.6, 38.9; of 1 x 16000 53.4, 52.6, 53.7; a chunk of 2 x 2048 behind 6000 452, 452, 461.
+// Of 16 powers of two, 2 kProducts are products and sums instead of the special-function unit's.  With 0, 1 and 2: trees of 8 sequences behind 2048
+// 39.5, 38.7, 39.0 us; of one behind 16000, 64 heads, 53.4, 53.8, 54.8; 64 sequences' tokens behind 4096 in pages of 128 154 each; a chunk 508, 524, 536.
 constexpr int kProducts = 1;
 constexpr int kTries = 1 << 20;             // of a wait, 3900 cycles each: after two seconds the block gives up (but see goes_on)
 
@@ -298,7 +302,7 @@ __device__ __forceinline__ uint32_t milliseconds() {            // of 2^20 ns; n
 }
 
 // A wait has had its tries: it goes on while a warp does rows once more, which takes as long as their keys are many, and for two seconds behind that.  (Asked
-// only then: with the question in a wait's loop a chunk of 2 x 2048 tokens behind 6000 took 531 us instead of 517.)
+// only then: with the question in a wait's loop a chunk took 531 us instead of 517.)
 template <int D>
 __device__ __noinline__ bool goes_on(Shared<D> &sh) {
   if (tries_of(sh) != kTries) return false;
@@ -910,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const __grid_
     auto arrived = [&](uint64_t *bar, uint32_t parity) { return warp_wait(sh, bar, parity); };
     // How a tile lies: 64 elements of its 128 keys after the other 64; or, folded, page by page both halves, 8 (16) keys each.  Of folded pages of 16 the
     // first 8 keys of all pages are one product's columns and the others another's, and the columns come in this order.  (The first way has its offsets
-    // in the instructions: with them in registers a chunk of 2 x 2048 tokens behind 6000 took 482 instead of 456 us.)
+    // in the instructions: with them in registers a chunk took 6 % longer.)
     const uint64_t k_tile = tile_descriptor(ring, 1024, 16), v_tile = tile_descriptor(ring, 1024, kTile * 128);
     int box = 0;                            // bytes of a folded page; 0: the first way
     auto logits = [&](int s, int half, int buffer) {
@@ -1391,7 +1395,7 @@ struct CutList {
 };
 
 // Thread blocks with numbers side by side often come to one multiprocessor, the first that has room: few items go to numbers far apart.  (A token of 32 heads
-// behind 3000 others takes 18 us so, 28 with item i in thread block i.)
+// behind 3000 others takes 15.1 us so, 19.6 with item i in thread block i.)
 __device__ __forceinline__ int first_item(const Params &p) { return (int)(blockIdx.x * (unsigned)p.join_step % gridDim.x); }
 
 // An item: 32 rows, half the columns; a row a lane, D / 16 columns a warp.
@@ -1551,7 +1555,7 @@ cudaError_t launch_attention(const Params &p, const Maps &maps, int sms, cudaStr
   if (e == cudaSuccess) e = launch_chained(attend_tiles_kernel<T, D>, dim3(sms), dim3(kThreads), smem, s, maps, p);
   if (e == cudaSuccess && p.split) {
     const long long rows = (long long)p.a.max_queries * p.group;
-    // (a token of 32 heads behind 6000 others: 17.0 us with the first, 29.8 with the second)
+    // (a token of 32 heads behind 6000 others: 17.5 us with the first, 31.3 with the second)
     if (rows <= 32) e = launch_chained(join_few_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
     else e = launch_chained(join_parts_kernel<T, D>, dim3(kJoinBlocks * sms), dim3(kJoinThreads), 0, s, p);
   }
@@ -1590,10 +1594,10 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
   p.group_inverse = p.group > 1 ? (uint32_t)((0x100000000ull + p.group - 1) / p.group) : 0;
   p.blocks_per_seq = (int)blocks;
   p.box_rows = p.c.page_size < kTile ? p.c.page_size : kTile;
-  // (tiles of all blocks of rows are counted in 32 bits; with whole blocks 64 sequences' tokens behind 4096 in pages of 16 take 184 us instead of 153)
+  // (tiles of all blocks of rows are counted in 32 bits; with whole blocks 64 sequences' tokens behind 4096 take 196 us instead of 174)
   p.split = blocks * p.c.batch <= kMaxPairs && blocks * p.c.batch * p.c.kv_heads * ((int64_t)p.c.max_pages * p.c.page_size / kTile + 1) <= 0x7FFFFFFF;
-  // Equal pieces against an even deal: 8 trees of 60 nodes, 32 heads, behind 2048 tokens take 38.8 us and 41.2, a token of 32
-  // heads behind 6000 others 17.0 and 20.5.  A piece of fewer tiles than these costs more to join than it saves: 8 such trees behind 300 take 23.7 us with pieces of 2 tiles, 20.2 of 3.
+  // Equal pieces against an even deal: trees of 8 sequences behind 2048 take 38.7 us and 41.7, a token of 32
+  // heads behind 6000 others 17.5 and 21.1.  A piece of fewer tiles than these costs more to join than it saves: 8 trees behind 300 take 23.8 us with pieces of 2 tiles, 20.2 of 3.
   p.least_tiles = rows > kRows ? 3 : 2;
 #ifdef C2T_DEBUG_BOUNDS
   p.tries = c2t_debug_attention_wait_limit;
@@ -1610,12 +1614,12 @@ int c2t_verify_attention(const c2t_cache *cache, const c2t_attention *attention,
     cudaGetLastError();
     return C2T_ECUDA;
   }
-  // By copies where the groups of heads divide a copy's rows and no dimension is without a stride, as broadcast queries have: windows of 1024, 16 sequences of 64
-  // heads, take 75.6 us, thread by thread 79.1; trees of 32 x 3000 121.5 and 124.2; a chunk 452 and 453.
+  // By copies where the groups of heads divide a copy's rows and no dimension is without a stride, as broadcast queries have: a window takes 76 us, thread by
+  // thread 81; trees of 32 sequences behind 3000 135.5 and 133.6; a chunk 524 and 517.
   const bool strides = (p.c.batch == 1 || p.a.q_seq_stride > 0) && (p.a.max_queries == 1 || p.a.q_token_stride > 0) && (p.a.q_heads == 1 || p.a.q_head_stride > 0);
   p.copy_queries = strides && p.group <= kQueryRows && (p.group & (p.group - 1)) == 0 && encode_queries(p.c, p.a, p.group, &maps.q);
-  // Copies of 2 KB are dealt with at 140 cycles each, which is less than the memory gives.  With both halves of a head in one, 64 sequences' tokens behind 4096 in
-  // pages of 16 take 152 us instead of 185, trees of 32 x 3000 256 instead of 291.  (The logits are two products of half the columns each then, which blocks of
+  // Copies of 2 KB are dealt with at 140 cycles each, which is less than the memory gives.  With both halves of a head in one, 64 sequences' tokens behind 4096
+  // take 174 us instead of 192, trees of 32 sequences behind 3000 with 32 key heads 304 instead of 325.  (The logits are two products of half the columns each then, which blocks of
   // more than 128 rows would wait for: they take pages half by half.)
   p.folded = p.c.head_dim == 128 && p.c.page_size <= 16 && encode_folded(p.c, p.c.k_dev, p.a.layer, &maps.k_folded) &&
              encode_folded(p.c, p.c.v_dev, p.a.layer, &maps.v_folded);

@@ -103,6 +103,8 @@ class KVCache:
     order of the others: `permute` a pool that is laid out head by head).  table: [batch, max_pages] int32, held: [batch] int32, refs:
     [n_pages] int32; `new_state` makes them for an empty cache.  q_heads, max_queries: the largest attention call that will
     be made; without them the cache has no workspace and its other calls work.  One thread at a time makes calls, as on a context.
+    status and workspace are made on the stream that is current here: a call on another one waits for it first, as for the caller's own tensors, and the
+    object outlives the work and the graphs that use it.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, held: torch.Tensor, refs: torch.Tensor,
