@@ -174,12 +174,14 @@ constexpr int kQueryRows = 32;              // rows of queries that one copy bri
 struct Block {                              // with the tiles [k0, k1) of it that a thread block takes
   int b, head, row0, rows;                  // key head; first row; rows that are there (0: no block)
   int prefix, n, keys;                      // of the sequence, as in Sight
-  int sink_tiles, first_tile, tiles, k0, k1;
-  // Long blocks begin with the second tile, go on to the last, and end with the first and the sinks': of those a row with a window may see a few keys only,
-  // and its maximum would have to be raised behind them.  (With the sinks first and the others in ascending order a window takes 95 us, with the sinks last 90, so 76.)
+  int tiles, k0, k1;
+  // The tiles' order: `bulk` of them side by side, from key bulk_key on, then the one at last_key, then the sinks'.  With a window of three tiles and more
+  // the bulk begins with the second and the first comes behind it, else it is all of them: of the first tile and the sinks' a row may see a few keys only, and
+  // its maximum would have to be raised behind them.  (With the sinks first and the others in ascending order a window takes 95 us, with the sinks last 90, so 76.)
+  int bulk, bulk_key, last_key;
   __device__ __forceinline__ int key0(int t) const {
-    const int near = tiles - sink_tiles;
-    return (t >= near ? t - near : near <= 2 ? first_tile + t : first_tile + (t + 1 < near ? t + 1 : 0)) * kTile;
+    const int behind = t - bulk;
+    return behind < 0 ? bulk_key + t * kTile : behind > 0 || last_key < 0 ? (behind - (last_key < 0 ? 0 : 1)) * kTile : last_key;
   }
 };
 
@@ -190,17 +192,26 @@ __device__ __forceinline__ Block block_of(const Params &p, int pair) {
   const Sight s = sight_of(p.c, p.a, w.b);
   w.prefix = s.prefix; w.n = s.n; w.keys = s.keys;
   w.rows = min(max(s.n * p.group - w.row0, 0), kBlockRows);
-  w.sink_tiles = w.first_tile = w.tiles = w.head = w.k0 = w.k1 = 0;
+  w.tiles = w.head = w.k0 = w.k1 = w.bulk = w.bulk_key = 0;
+  w.last_key = -1;
   if (w.rows == 0) return w;
-  const int first = token_of(p, w.row0), last = token_of(p, w.row0 + w.rows - 1);
+  const int first_token = token_of(p, w.row0), last = token_of(p, w.row0 + w.rows - 1);
   const int end = s.bits ? s.keys : min(s.keys, s.prefix + last + 1);
   const int end_tile = (end + kTile - 1) / kTile;
+  int sinks = 0, first = 0;                 // tiles that hold sinks; the first one that a row's window can reach
   if (s.window > 0) {
-    const int lowest = s.prefix + (s.positions ? 0 : first);                    // the lowest position of a row
-    w.first_tile = min(max(lowest - s.window + 1, 0) / kTile, max(end_tile - 1, 0));
-    w.sink_tiles = min((min(s.sinks, end) + kTile - 1) / kTile, w.first_tile);
+    const int lowest = s.prefix + (s.positions ? 0 : first_token);              // the lowest position of a row
+    first = min(max(lowest - s.window + 1, 0) / kTile, max(end_tile - 1, 0));
+    sinks = min((min(s.sinks, end) + kTile - 1) / kTile, first);
   }
-  w.tiles = max(w.sink_tiles + end_tile - w.first_tile, 1);                     // (rows that see nothing are written too)
+  w.bulk = max(end_tile - first, 1);                                            // (rows that see nothing are written too)
+  w.bulk_key = first * kTile;
+  w.tiles = sinks + w.bulk;
+  if (s.window > 0 && w.bulk > 2) {
+    w.last_key = w.bulk_key;
+    w.bulk_key += kTile;
+    --w.bulk;
+  }
   return w;
 }
 
